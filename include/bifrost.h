@@ -305,6 +305,132 @@ int bf_get_key_stream_bytes(bf_ctx* ctx, uint64_t* distinct_out, uint64_t* per_r
  * once per launch).  Resets the counter.  Does not synchronise. */
 int bf_get_mac_key_bytes(bf_ctx* ctx, uint64_t* out);
 
+/* ------------------------------------------------------------------------------------------------
+ * The trusted half of a decode step.
+ *
+ * What follows works on PLAINTEXT and belongs on a GPU of the trusted domain (Sec. 3.2: attention and KV-state transitions
+ * stay there; Sec. 3.5 keeps the KV state as the trusted side's own), next to bf_linear, which works on ciphertexts on an
+ * untrusted one.  Between two encrypted products a decoder appends new keys and values to its cache and attends over it;
+ * behind the last layer it projects onto the vocabulary.  Both are bound by memory, so both are held in 4 bits with group
+ * scales.  All conventions at the head of this file hold, with bf_trusted in the place of bf_ctx; and
+ *   - no call allocates, frees or synchronises unless stated, so every one can be captured into a CUDA graph.  Graphs
+ *     captured from one bf_trusted share its workspace: replay them on one stream in turn, or give each a bf_trusted.
+ *   - the calling thread's current device may be any: calls switch to the context's device and back.
+ *   - indices that live in device memory (pages, sequences, lengths) are checked by the kernels.  What a bad one would have
+ *     reached is left alone, and bf_trusted_status reports it.
+ */
+typedef struct bf_trusted bf_trusted;  /* stream, status word, workspace */
+
+/* workspace_bytes: 0 = 32 MiB; at least 1 MiB.  Partial results of split attention and lists of pages live there; a call that
+ * needs more than there is returns BF_ERR_TOO_LARGE and enqueues nothing.  Allocates; synchronises.  Errors: INVALID_ARG, OOM, CUDA. */
+int bf_trusted_create(bf_trusted** out, uint64_t workspace_bytes, void* cuda_stream);
+void bf_trusted_destroy(bf_trusted* t);                       /* synchronises */
+/* Synchronises the stream, returns what the kernels found since the last call, and forgets it: BF_ERR_RANGE (an index or a
+ * length in device memory was out of range, a list named a sequence twice where that has no meaning, a reference count went
+ * below zero), else BF_ERR_OOM (the pool ran out of pages), else BF_OK.  INVALID_ARG while the stream is being captured. */
+int bf_trusted_status(bf_trusted* t);
+const char* bf_trusted_last_cuda_error(const bf_trusted* t);
+
+enum { BF_F32 = 0, BF_F16 = 1, BF_BF16 = 2 };
+
+/* Rows of activations in device memory: element (row, head, channel) at data + row * row_stride + head * head_stride + channel, in
+ * elements of the type.  Strides may be any (rows of q, k and v may lie in one array); head_stride is not used where rows have no heads. */
+typedef struct {
+    void* data;
+    int64_t row_stride, head_stride;
+    int32_t type;                          /* BF_F32, BF_F16 or BF_BF16 */
+} bf_rows;
+
+/* A weight matrix in 4 bits: W[o][c] = scales[o][c / group] * (code[o][c] - 8) + offsets[o][c / group].
+ *   codes    device, 16-byte aligned, [d_out][row_bytes]: column c in bits 4*(c%2) .. of byte c/2; row_bytes is a multiple of 16 and
+ *            holds d_in codes (what lies behind them is not used)
+ *   scales   device, 16-byte aligned, fp16 [d_out][group_stride], group_stride a multiple of 8, at least ceil(d_in / group)
+ *   offsets  the same, or NULL for none
+ *   group    32, 64 or 128 */
+typedef struct {
+    const uint8_t* codes;
+    const void* scales;
+    const void* offsets;
+    uint64_t row_bytes;
+    uint32_t group_stride, d_out, d_in, group;
+} bf_q4_matrix;
+
+/* y[i] = W x[i] for n rows: the plaintext counterpart of bf_linear, for projections that stay in the trusted domain (the
+ * vocabulary).  Products are of the 4-bit codes themselves, sums in 32 bits, one rounding to the type of y.  x may be any type,
+ * y another.  A non-finite x makes its row of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, CUDA. */
+int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y);
+
+/* Keys and values of n_seqs sequences in pages of page_tokens tokens (16 to 256, a multiple of 16), one page holding a run of
+ * tokens of ONE sequence, for all layers.  An element is low + scale * code, both fp16, per token, head and `group` channels.
+ *   pool     device, 16-byte aligned, [n_layers][n_pages][n_kv_heads][bf_kv4_block_bytes]
+ *   tables   device, [n_seqs][max_pages]: the page of tokens page_tokens*i .. of a sequence, -1 where there is none
+ *   lengths  device, [n_seqs]: tokens of each sequence
+ *   refs     device, [n_pages]: how many tables name a page; 0 = free.  A page that is not full has one owner.
+ * A block is page_tokens/16 sub-blocks of 16 tokens, each
+ *     key codes     16*D/2 bytes    channel c of token u: nibble c%8 of word (u/8) + 2*(c/32%2) + 4*(c/8%4) + 16*(u%8) + 128*(c/64)
+ *     key pars      64*D/group      fp16 (scale, low) of token u, group e: pair e + (D/group)*(u/8 + 2*(u%8))
+ *     value codes   16*D/2          nibble c/8%2 + 2*(u/8) + 4*(u%2) of word (c/16%4) + 4*(u/2%4) + 16*(c%8) + 128*(c/64)
+ *     value pars    64*D/group      fp16 scale at u%2 + 2*(u/8) + 8*(u/2%4) + 32*e, low 4 behind it
+ * i.e. the order in which the matrix instructions of bf_kv4_attention take them. */
+typedef struct {
+    void* pool;
+    int32_t* tables;
+    int32_t* lengths;
+    int32_t* refs;
+    uint32_t n_layers, n_pages, n_kv_heads, head_dim, group, page_tokens, n_seqs, max_pages;
+} bf_kv4_cache;
+
+/* Bytes of one page of one layer and head: (16*D + 128*D/group) * page_tokens/16.  0 where the combination is not held: head_dim is
+ * 64 or 128, group 32, 64 or 128 and at most head_dim, page_tokens a multiple of 16 from 16 to 256. */
+uint64_t bf_kv4_block_bytes(uint32_t head_dim, uint32_t group, uint32_t page_tokens);
+
+/* Lists of sequences below: `seqs` (device, int32 [n]; NULL = 0 .. n-1) names them, `starts` (device, int32 [n+1], ascending; NULL = one
+ * row each) says that rows starts[i] .. starts[i+1]-1 of q, k, v or out belong to sequence seqs[i]: its LAST tokens.  Rows behind
+ * starts[n] are not touched. */
+
+/* Pages for counts[i] (device, int32 [n]; NULL = 1) more tokens of each sequence, lowest free pages first, in the order of the list;
+ * lengths grow by that.  A sequence for which no pages are left (OOM), that would exceed its table or is named twice (RANGE: the
+ * first one counts) keeps its length; one that needs no new page is always served.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+int bf_kv4_grow(bf_trusted* t, const bf_kv4_cache* c, const int32_t* seqs, const int32_t* counts, uint32_t n);
+
+/* Quantises rows of k and v ([head][channel], any type) as the last tokens of their sequences in one layer.  Values are clamped to
+ * +-61440; scale = (max - min) / 15, low = min, rounded to fp16 by way of fp32; code = round((x - low) / scale), ties to even, decided as in 64
+ * bits.  A group with a NaN reads as NaN.  max_new bounds the rows of a sequence (one with more is RANGE and left alone).
+ * Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+int bf_kv4_append(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int32_t* seqs, const int32_t* starts, uint32_t n,
+                  uint32_t max_new, const bf_rows* k, const bf_rows* v);
+
+/* The reverse: tokens first[i] .. (device, int32 [n]; NULL = the last ones) of each sequence as rows of k and v. */
+int bf_kv4_read(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int32_t* seqs, const int32_t* starts, const int32_t* first,
+                uint32_t n, uint32_t max_tokens, const bf_rows* k, const bf_rows* v);
+
+/* Attention of one layer over the cache.  Row starts[i] + j of q ([head][channel], fp16 or bf16; n_q_heads a multiple of n_kv_heads,
+ * query head h reads key head h / (n_q_heads / n_kv_heads)) stands at position p = length - (its sequence's rows) + j and sees tokens
+ *     max(0, p - window + 1) .. p          (window = 0: from 0)
+ *     out = sum_t softmax_t(scale * <q, K_t>) V_t
+ * Cache values behind a sequence's length are never used, whatever they are.  A row that sees nothing (an empty sequence, more rows
+ * than tokens) becomes zeros.  lse (device, fp32 [rows][n_q_heads], or NULL) receives log sum exp, -inf for such a row: results
+ * over several caches are joined with it.  Products with the codes are exact, scores, softmax and sums in 32 bits; probabilities
+ * and values enter the second product in fp16 (half a step, 2^-11, of each).
+ * max_q: most rows of a sequence (one with more is RANGE, its rows are left alone); max_len: a length that the work is
+ * divided for (any is right).  out: the type of q, any strides; it may not overlap q.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+int bf_kv4_attention(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int32_t* seqs, const int32_t* starts, uint32_t n,
+                     uint32_t max_q, uint32_t max_len, const bf_rows* q, uint32_t n_q_heads, const bf_rows* out, float scale,
+                     uint32_t window, float* lse);
+
+/* Sequence dst[i] (empty before) becomes a copy of src[i]: full pages are shared, a last page that is not full is copied in every
+ * layer.  Both lists device, int32 [n].  A dst that is not empty, named twice (the first one counts), or whose src is a dst too is RANGE and
+ * stays as it is; one for whose copy no page is left is OOM and stays empty.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+int bf_kv4_fork(bf_trusted* t, const bf_kv4_cache* c, const int32_t* src, const int32_t* dst, uint32_t n);
+
+/* Empties sequences (device, int32 [n]): their pages lose a reference each.  Naming one twice frees it once. */
+int bf_kv4_free(bf_trusted* t, const bf_kv4_cache* c, const int32_t* seqs, uint32_t n);
+
+/* Moves live pages to the front of the pool: the k-th live page at or behind the number of live pages goes to the k-th free one
+ * before it, in every layer.  tables_out, refs_out: where the new tables and counts go (NULL = in place; else arrays apart from the
+ * cache's own, of the same size).  n_live (device, int32, or NULL) receives the number of live pages. */
+int bf_kv4_compact(bf_trusted* t, const bf_kv4_cache* c, int32_t* tables_out, int32_t* refs_out, int32_t* n_live);
+
 const char* bf_strerror(int code);
 const char* bf_last_cuda_error(const bf_ctx* ctx);
 

@@ -36,6 +36,69 @@ class bf_plan(ctypes.Structure):
                 ("bsgs_b", ctypes.c_uint32), ("bsgs_g", ctypes.c_uint32), ("flags", ctypes.c_uint32)]
 
 
+BF_F32 = 0
+BF_F16 = 1
+BF_BF16 = 2
+
+
+def _type_of(tensor) -> int:
+    name = str(tensor.dtype)
+    types = {"torch.float32": BF_F32, "torch.float16": BF_F16, "torch.bfloat16": BF_BF16}
+    if name not in types:
+        raise ValueError(f"rows are float32, float16 or bfloat16, not {name}")
+    return types[name]
+
+
+def _dense(tensor, dtype: str, what: str):
+    if str(tensor.dtype) != dtype or not tensor.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor is wanted")
+    return tensor.data_ptr()
+
+
+class bf_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+    @classmethod
+    def of(cls, tensor):
+        """Rows [n][channels] or [n][heads][channels] of a tensor, which must live as long; any strides but the channels'."""
+        if tensor.dim() not in (2, 3) or (tensor.stride(-1) != 1 and tensor.shape[-1] != 1):
+            raise ValueError("rows are [n][channels] or [n][heads][channels] with the channels side by side")
+        return cls(tensor.data_ptr(), tensor.stride(0), tensor.stride(1) if tensor.dim() == 3 else 0, _type_of(tensor))
+
+
+class bf_q4_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("row_bytes", ctypes.c_uint64),
+                ("group_stride", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("d_in", ctypes.c_uint32), ("group", ctypes.c_uint32)]
+
+    @classmethod
+    def of(cls, codes, scales, offsets, d_in: int, group: int):
+        """codes uint8 [d_out][row_bytes], scales (and offsets, or None) float16 [d_out][group_stride]; they must live as long."""
+        if offsets is not None and offsets.shape != scales.shape:
+            raise ValueError("offsets have the shape of the scales")
+        if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
+            raise ValueError("codes and scales have a row for each output")
+        return cls(_dense(codes, "torch.uint8", "codes"), _dense(scales, "torch.float16", "scales"),
+                   None if offsets is None else _dense(offsets, "torch.float16", "offsets"), codes.shape[1], scales.shape[1], codes.shape[0],
+                   d_in, group)
+
+
+class bf_kv4_cache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p)] + \
+               [(name, ctypes.c_uint32) for name in ("n_layers", "n_pages", "n_kv_heads", "head_dim", "group", "page_tokens", "n_seqs", "max_pages")]
+
+    @classmethod
+    def of(cls, pool, tables, lengths, refs, head_dim: int, group: int, page_tokens: int):
+        """pool uint8 [layers][pages][kv heads][block bytes], tables int32 [seqs][max_pages], lengths int32 [seqs], refs int32 [pages];
+        they must live as long."""
+        layers, pages, heads, block = pool.shape
+        if block != bf_kv4_block_bytes(head_dim, group, page_tokens):
+            raise BifrostError(BF_ERR_SHAPE, "bf_kv4_cache", f"a block of {block} bytes")
+        if tables.dim() != 2 or lengths.shape != tables.shape[:1] or refs.shape != pool.shape[1:2]:
+            raise BifrostError(BF_ERR_SHAPE, "bf_kv4_cache", "tables, lengths and refs do not fit together")
+        return cls(_dense(pool, "torch.uint8", "pool"), _dense(tables, "torch.int32", "tables"), _dense(lengths, "torch.int32", "lengths"),
+                   _dense(refs, "torch.int32", "refs"), layers, pages, heads, head_dim, group, page_tokens, tables.shape[0], tables.shape[1])
+
+
 class BifrostError(RuntimeError):
     def __init__(self, code: int, where: str, detail: str = ""):
         self.code = code
@@ -85,6 +148,19 @@ _SIGNATURES = {
     "bf_measure_fma64_rate": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_double)]),
     "bf_get_key_stream_bytes": (ctypes.c_int, [_vp, ctypes.POINTER(_u64), ctypes.POINTER(_u64)]),
     "bf_get_mac_key_bytes": (ctypes.c_int, [_vp, ctypes.POINTER(_u64)]),
+    "bf_trusted_create": (ctypes.c_int, [ctypes.POINTER(_vp), _u64, _vp]),
+    "bf_trusted_destroy": (None, [_vp]),
+    "bf_trusted_status": (ctypes.c_int, [_vp]),
+    "bf_trusted_last_cuda_error": (ctypes.c_char_p, [_vp]),
+    "bf_q4_linear": (ctypes.c_int, [_vp, _vp, _vp, _u32, _vp]),
+    "bf_kv4_block_bytes": (_u64, [_u32, _u32, _u32]),
+    "bf_kv4_grow": (ctypes.c_int, [_vp, _vp, _vp, _vp, _u32]),
+    "bf_kv4_append": (ctypes.c_int, [_vp, _vp, _u32, _vp, _vp, _u32, _u32, _vp, _vp]),
+    "bf_kv4_read": (ctypes.c_int, [_vp, _vp, _u32, _vp, _vp, _vp, _u32, _u32, _vp, _vp]),
+    "bf_kv4_attention": (ctypes.c_int, [_vp, _vp, _u32, _vp, _vp, _u32, _u32, _u32, _vp, _u32, _vp, ctypes.c_float, _u32, _vp]),
+    "bf_kv4_fork": (ctypes.c_int, [_vp, _vp, _vp, _vp, _u32]),
+    "bf_kv4_free": (ctypes.c_int, [_vp, _vp, _vp, _u32]),
+    "bf_kv4_compact": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp]),
     "bf_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "bf_last_cuda_error": (ctypes.c_char_p, [_vp]),
 }
@@ -318,3 +394,76 @@ def bf_get_mac_key_bytes(ctx) -> int:
     a = _u64(0)
     _check(load().bf_get_mac_key_bytes(ctx, ctypes.byref(a)), "bf_get_mac_key_bytes", ctx)
     return int(a.value)
+
+
+# ---- the trusted half: descriptors (bf_rows, bf_q4_matrix, bf_kv4_cache) are passed by reference, lists as int32 tensors or None
+
+def _check_trusted(code: int, where: str, t):
+    if code != BF_OK:
+        detail = (load().bf_trusted_last_cuda_error(t) or b"").decode() if code == BF_ERR_CUDA and t else ""
+        raise BifrostError(code, where, detail)
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.addressof(struct)
+
+
+def _list(x):
+    if x is not None and not isinstance(x, int):
+        return _dense(x, "torch.int32", "a list")
+    return x
+
+
+def bf_trusted_create(workspace_bytes: int = 0, cuda_stream: int = 0):
+    out = _vp()
+    _check_trusted(load().bf_trusted_create(ctypes.byref(out), workspace_bytes, cuda_stream), "bf_trusted_create", None)
+    return out
+
+
+def bf_trusted_destroy(t):
+    load().bf_trusted_destroy(t)
+
+
+def bf_trusted_status(t):
+    """Synchronises; raises what the kernels found wrong in device memory since the last call."""
+    _check_trusted(load().bf_trusted_status(t), "bf_trusted_status", t)
+
+
+def bf_q4_linear(t, W: bf_q4_matrix, x: bf_rows, n: int, y: bf_rows):
+    _check_trusted(load().bf_q4_linear(t, _ref(W), _ref(x), n, _ref(y)), "bf_q4_linear", t)
+
+
+def bf_kv4_block_bytes(head_dim: int, group: int, page_tokens: int) -> int:
+    return load().bf_kv4_block_bytes(head_dim, group, page_tokens)
+
+
+def bf_kv4_grow(t, cache: bf_kv4_cache, seqs, counts, n: int):
+    _check_trusted(load().bf_kv4_grow(t, _ref(cache), _list(seqs), _list(counts), n), "bf_kv4_grow", t)
+
+
+def bf_kv4_append(t, cache: bf_kv4_cache, layer: int, seqs, starts, n: int, max_new: int, k: bf_rows, v: bf_rows):
+    _check_trusted(load().bf_kv4_append(t, _ref(cache), layer, _list(seqs), _list(starts), n, max_new, _ref(k), _ref(v)), "bf_kv4_append", t)
+
+
+def bf_kv4_read(t, cache: bf_kv4_cache, layer: int, seqs, starts, first, n: int, max_tokens: int, k: bf_rows, v: bf_rows):
+    _check_trusted(load().bf_kv4_read(t, _ref(cache), layer, _list(seqs), _list(starts), _list(first), n, max_tokens, _ref(k), _ref(v)),
+                   "bf_kv4_read", t)
+
+
+def bf_kv4_attention(t, cache: bf_kv4_cache, layer: int, seqs, starts, n: int, max_q: int, max_len: int, q: bf_rows, n_q_heads: int,
+                     out: bf_rows, scale: float, window: int = 0, lse=None):
+    _check_trusted(load().bf_kv4_attention(t, _ref(cache), layer, _list(seqs), _list(starts), n, max_q, max_len, _ref(q), n_q_heads,
+                                           _ref(out), scale, window, None if lse is None else _dense(lse, "torch.float32", "lse")),
+                   "bf_kv4_attention", t)
+
+
+def bf_kv4_fork(t, cache: bf_kv4_cache, src, dst, n: int):
+    _check_trusted(load().bf_kv4_fork(t, _ref(cache), _list(src), _list(dst), n), "bf_kv4_fork", t)
+
+
+def bf_kv4_free(t, cache: bf_kv4_cache, seqs, n: int):
+    _check_trusted(load().bf_kv4_free(t, _ref(cache), _list(seqs), n), "bf_kv4_free", t)
+
+
+def bf_kv4_compact(t, cache: bf_kv4_cache, tables_out=None, refs_out=None, n_live=None):
+    _check_trusted(load().bf_kv4_compact(t, _ref(cache), _list(tables_out), _list(refs_out), _list(n_live)), "bf_kv4_compact", t)

@@ -7,8 +7,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbifrost.so")
-SOURCES = ["api.cu", "ntt.cu", "kernels.cu", "mac.cu", "mac_wide.cu", "encode.cu"]
-HEADERS = ["bf_common.cuh", "bf_host.h", "mac_kernel.cuh", os.path.join("..", "..", "include", "bifrost.h")]
+SOURCES = ["api.cu", "ntt.cu", "kernels.cu", "mac.cu", "mac_wide.cu", "encode.cu", "trusted.cu", "q4.cu", "kv4.cu"]
+HEADERS = ["bf_common.cuh", "bf_host.h", "mac_kernel.cuh", "bf_trusted.h", os.path.join("..", "..", "include", "bifrost.h")]
 
 
 def _stale() -> bool:

@@ -1,0 +1,782 @@
+"""The trusted half (4-bit products, the 4-bit cache and its pages): refusals on the CPU, numerics against 64 bits on the GPU."""
+import ctypes
+import itertools
+
+import numpy as np
+import pytest
+
+from paper_2606_17421_b200 import bifrost as bf
+from tests import trusted_ref as ref
+
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ refusals, without a device
+
+@pytest.fixture
+def stand_in():
+    """A context that no call gets to use: arguments are looked at first, then the device, which there need not be."""
+    from paper_2606_17421_b200 import build
+    build.build()
+    return ctypes.create_string_buffer(4096)
+
+
+def matrix(**kw):
+    d = dict(codes=4096, scales=4096, offsets=None, row_bytes=48, group_stride=8, d_out=10, d_in=90, group=32)
+    return bf.bf_q4_matrix(**{**d, **kw})
+
+
+def rows(**kw):
+    return bf.bf_rows(**{**dict(data=4096, row_stride=128, head_stride=64, type=bf.BF_BF16), **kw})
+
+
+def cache(**kw):
+    d = dict(pool=4096, tables=4096, lengths=4096, refs=4096, n_layers=2, n_pages=8, n_kv_heads=2, head_dim=64, group=32, page_tokens=32,
+             n_seqs=3, max_pages=4)
+    return bf.bf_kv4_cache(**{**d, **kw})
+
+
+def refused(code, call, *args):
+    with pytest.raises(bf.BifrostError) as ei:
+        call(*args)
+    assert ei.value.code == code, ei.value
+
+
+BAD_MATRIX = [(dict(codes=None), -1), (dict(codes=4104), -1), (dict(scales=None), -1), (dict(scales=4100), -1), (dict(offsets=4098), -1), (dict(d_out=0), -1),
+              (dict(d_in=0), -1), (dict(group=16), -3), (dict(group=0), -3), (dict(group=48), -3), (dict(row_bytes=40), -3), (dict(row_bytes=32), -3),
+              (dict(group_stride=4), -3), (dict(d_in=500, row_bytes=256), -3), (dict(d_out=2 ** 31), -3), (dict(d_in=2 ** 32 - 1, row_bytes=2 ** 31, group_stride=2 ** 27), -3)]
+
+
+@pytest.mark.parametrize("change,code", BAD_MATRIX, ids=str)
+def test_linear_refuses_matrices(stand_in, change, code):
+    refused(code, bf.bf_q4_linear, stand_in, matrix(**change), rows(), 1, rows())
+
+
+def test_linear_refuses_rows_and_counts(stand_in):
+    for bad in (dict(data=None), dict(type=3), dict(type=-1), dict(data=4097), dict(data=4098, type=bf.BF_F32)):
+        refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, stand_in, matrix(), rows(**bad), 1, rows())
+        refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, stand_in, matrix(), rows(), 1, rows(**bad))
+    refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, stand_in, matrix(), rows(), 0, rows())
+    refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, None, matrix(), rows(), 1, rows())
+    refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, stand_in, None, rows(), 1, rows())
+    refused(bf.BF_ERR_INVALID_ARG, bf.bf_q4_linear, stand_in, matrix(), None, 1, rows())
+    refused(bf.BF_ERR_SHAPE, bf.bf_q4_linear, stand_in, matrix(), rows(), 2 ** 31, rows())
+
+
+BAD_CACHE = [(dict(pool=None), -1), (dict(pool=4104), -1), (dict(tables=None), -1), (dict(tables=4098), -1), (dict(lengths=None), -1), (dict(refs=None), -1),
+             (dict(n_layers=0), -1), (dict(n_pages=0), -1), (dict(n_kv_heads=0), -1), (dict(n_seqs=0), -1), (dict(max_pages=0), -1), (dict(head_dim=96), -3),
+             (dict(head_dim=256), -3), (dict(group=16), -3), (dict(group=128), -3), (dict(page_tokens=24), -3), (dict(page_tokens=0), -3), (dict(page_tokens=512), -3),
+             (dict(max_pages=2 ** 27), -3), (dict(n_pages=2 ** 31), -3), (dict(n_kv_heads=5000), -3), (dict(n_layers=2 ** 17), -3), (dict(n_pages=2 ** 30, n_kv_heads=1000), -3)]
+
+
+@pytest.mark.parametrize("change,code", BAD_CACHE, ids=str)
+def test_every_call_refuses_bad_caches(stand_in, change, code):
+    c, r = cache(**change), rows()
+    refused(code, bf.bf_kv4_grow, stand_in, c, None, None, 1)
+    refused(code, bf.bf_kv4_append, stand_in, c, 0, None, None, 1, 1, r, r)
+    refused(code, bf.bf_kv4_read, stand_in, c, 0, None, None, None, 1, 1, r, r)
+    refused(code, bf.bf_kv4_attention, stand_in, c, 0, None, None, 1, 1, 1, r, 2, r, 1.0, 0, None)
+    refused(code, bf.bf_kv4_fork, stand_in, c, 4096, 8192, 1)
+    refused(code, bf.bf_kv4_free, stand_in, c, 4096, 1)
+    refused(code, bf.bf_kv4_compact, stand_in, c, None, None, None)
+
+
+def test_cache_calls_refuse_arguments(stand_in):
+    c, r = cache(), rows()
+    inv, shape, large = bf.BF_ERR_INVALID_ARG, bf.BF_ERR_SHAPE, bf.BF_ERR_TOO_LARGE
+    att = lambda *a: bf.bf_kv4_attention(stand_in, *a)          # noqa: E731
+    for n, most in ((0, 1), (1, 0)):
+        refused(inv, bf.bf_kv4_append, stand_in, c, 0, None, None, n, most, r, r)
+        refused(inv, bf.bf_kv4_read, stand_in, c, 0, None, None, None, n, most, r, r)
+        refused(inv, att, c, 0, None, None, n, most, 1, r, 2, r, 1.0, 0, None)
+    refused(shape, bf.bf_kv4_append, stand_in, c, 2, None, None, 1, 1, r, r)                    # no such layer
+    refused(shape, bf.bf_kv4_append, stand_in, c, 0, None, None, 4, 1, r, r)                    # more than there are, unnamed
+    refused(shape, bf.bf_kv4_grow, stand_in, c, None, None, 4)
+    refused(inv, bf.bf_kv4_grow, stand_in, c, None, None, 0)
+    refused(large, bf.bf_kv4_append, stand_in, c, 0, 4096, 4096, 2 ** 20, 2 ** 20, r, r)
+    refused(inv, bf.bf_kv4_append, stand_in, c, 0, None, None, 1, 1, rows(type=5), r)
+    refused(inv, att, c, 0, None, None, 1, 1, 1, rows(type=bf.BF_F32), 2, rows(type=bf.BF_F32), 1.0, 0, None)
+    refused(inv, att, c, 0, None, None, 1, 1, 1, rows(type=bf.BF_F16), 2, r, 1.0, 0, None)      # out has another type
+    refused(inv, att, c, 0, None, None, 1, 1, 0, r, 2, r, 1.0, 0, None)
+    refused(inv, att, c, 0, None, None, 1, 1, 1, r, 2, r, float("nan"), 0, None)
+    refused(inv, att, c, 0, None, None, 1, 1, 1, r, 2, r, float("inf"), 0, None)
+    refused(shape, att, c, 0, None, None, 1, 1, 1, r, 3, r, 1.0, 0, None)
+    refused(shape, att, c, 0, None, None, 1, 1, 1, r, 0, r, 1.0, 0, None)
+    refused(inv, bf.bf_kv4_fork, stand_in, c, None, 4096, 1)
+    refused(inv, bf.bf_kv4_fork, stand_in, c, 4096, 4096, 0)
+    refused(inv, bf.bf_kv4_free, stand_in, c, None, 1)
+    refused(inv, bf.bf_kv4_free, stand_in, c, 4096, 0)
+    refused(large, bf.bf_kv4_fork, stand_in, c, 4096, 4096, 70000)
+    # (the stand-in has no workspace)
+    refused(large, bf.bf_kv4_compact, stand_in, c, None, None, None)
+    refused(large, bf.bf_kv4_grow, stand_in, c, None, None, 1)
+    assert bf.load().bf_trusted_create(None, 0, None) == inv
+    out = ctypes.c_void_p()
+    assert bf.load().bf_trusted_create(ctypes.byref(out), 1000, None) == inv and not out.value
+    refused(inv, bf.bf_trusted_status, None)
+    bf.bf_trusted_destroy(None)
+
+
+def test_block_bytes():
+    assert bf.bf_kv4_block_bytes(128, 64, 64) == 4 * (128 * 16 + 2 * 128)
+    assert bf.bf_kv4_block_bytes(64, 64, 16) == 64 * 16 + 128
+    for D, G, T in ((128, 32, 8), (64, 128, 16), (80, 16, 16), (128, 0, 16), (128, 32, 272)):
+        assert bf.bf_kv4_block_bytes(D, G, T) == 0
+
+
+def test_descriptors_refuse_tensors():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(4, 3, 64)
+    assert bf.bf_rows.of(x[:, :2]).row_stride == 192 and bf.bf_rows.of(x[0]).head_stride == 0
+    for bad in (x.int(), x.transpose(1, 2), x[0, 0]):
+        with pytest.raises(ValueError):
+            bf.bf_rows.of(bad)
+    codes, scales = torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(4, 8, dtype=torch.float16)
+    assert bf.bf_q4_matrix.of(codes, scales, None, 32, 32).row_bytes == 16
+    for c, s, o in ((codes.int(), scales, None), (codes, scales.float(), None), (codes[:3], scales, None), (codes, scales, scales[:, :4]), (codes.t(), scales, None)):
+        with pytest.raises(ValueError):
+            bf.bf_q4_matrix.of(c, s, o, 32, 32)
+    with pytest.raises(bf.BifrostError):
+        bf.bf_kv4_cache.of(torch.zeros(1, 2, 2, 100, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32),
+                           torch.zeros(2, dtype=torch.int32), 64, 32, 16)
+
+
+def test_reference_layout_fills_every_nibble_once():
+    for D, G in ((64, 32), (64, 64), (128, 32), (128, 64), (128, 128)):
+        kn, kp, vn, vp = ref.places(D, G)
+        nib = np.concatenate([kn.ravel(), vn.ravel()])
+        half = np.concatenate([kp.ravel(), kp.ravel() + 1, vp.ravel(), vp.ravel() + 4])
+        used = np.concatenate([nib, *(4 * half + i for i in range(4))])
+        assert len(used) == len(set(used.tolist())) == 2 * (16 * D + 128 * (D // G)) and used.max() == len(used) - 1
+
+
+# ------------------------------------------------------------------------------------------------ on the device
+
+class Side:
+    """A context on a stream of its own, and torch's type names."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        torch.cuda.set_device(0)
+        self.stream = torch.cuda.Stream()
+        torch.cuda.set_stream(self.stream)
+        self.t = bf.bf_trusted_create(0, self.stream.cuda_stream)
+        self.types = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+    def dev(self, a):
+        return self.torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+    def ints(self, a):
+        return None if a is None else self.dev(np.asarray(a, np.int32))
+
+    def host(self, x):
+        self.torch.cuda.synchronize()
+        return x.double().cpu().numpy() if x.is_floating_point() else x.cpu().numpy()
+
+
+@pytest.fixture(scope="module")
+def side():
+    s = Side()
+    yield s
+    bf.bf_trusted_destroy(s.t)
+
+
+HALF_STEP = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"fp32": 2.0 ** -149, "fp16": 2.0 ** -25, "bf16": 2.0 ** -134}
+
+
+def draw_matrix(rng, d_out, d_in, group, offsets):
+    groups, bytes_ = -(-d_in // group), -(-d_in // 32) * 16
+    packed = rng.integers(0, 256, (d_out, bytes_), dtype=np.uint8)                   # codes behind d_in are anything too
+    scales = rng.uniform(0.001, 0.01, (d_out, -(-groups // 8) * 8)).astype(np.float16)
+    offs = (rng.standard_normal(scales.shape) * 0.02).astype(np.float16) if offsets else None
+    for a in (scales, offs):
+        if a is not None:
+            a[:, groups:] = np.nan                                                   # behind the last group: not used
+    code = np.stack([packed & 15, packed >> 4], -1).reshape(d_out, -1)[:, :d_in].astype(np.float64)
+    g = np.arange(d_in) // group
+    W = scales[:, g].astype(np.float64) * (code - 8) + (offs[:, g].astype(np.float64) if offsets else 0)
+    # what a sum in 32 bits meets on its way: codes up to 15, taken back by eight times the sum of x
+    top = scales[:, g].astype(np.float64) * 23 + (np.abs(offs[:, g].astype(np.float64)) if offsets else 0)
+    return packed, scales, offs, W, top
+
+
+def linear_tolerance(x, y, top, ytype):
+    """Half a step of y's type; 2^-22 of the largest magnitude met for each of the d_in/16 additions of 16 products and a few
+    more a group; x taken to 2^-22 of itself or 2^-24 of the largest of its row."""
+    K = x.shape[1]
+    mag = np.abs(x) @ top.T
+    big = np.abs(x).max(1, keepdims=True) * top.sum(1)[None]
+    return HALF_STEP[ytype] * np.abs(y) + 2.0 ** -22 * (K / 16 + K / 32 + 24) * mag + 2.0 ** -24 * big + TINY[ytype]
+
+
+LINEAR = [(1, 64, 16, 32), (1, 64, 17, 64), (1, 1, 1, 32), (1, 33, 5, 128), (2, 200, 129, 64), (3, 768, 300, 128), (7, 1000, 77, 32), (8, 1024, 64, 128), (9, 96, 2500, 32),
+          (16, 2048, 130, 64), (17, 511, 33, 128), (31, 640, 50, 32), (33, 1500, 100, 64), (64, 256, 1000, 128), (65, 320, 47, 64), (130, 160, 40, 32), (1, 14336, 40, 128),
+          (5, 9000, 20, 64), (40, 5000, 24, 128)]
+
+
+@gpu
+@pytest.mark.parametrize("n,d_in,d_out,group", LINEAR)
+def test_linear_against_64_bits(side, n, d_in, d_out, group):
+    torch = side.torch
+    for i, (xt, yt, offsets) in enumerate(itertools.product(("bf16", "fp16", "fp32"), ("bf16", "fp16", "fp32"), (False, True))):
+        rng = np.random.default_rng([n, d_in, d_out, i])
+        packed, scales, offs, W, top = draw_matrix(rng, d_out, d_in, group, offsets)
+        x = torch.from_numpy(rng.standard_normal((n, d_in)) * rng.choice([1, 1, 1, 8], d_in)).to(side.types[xt]).cuda()
+        y = torch.full((n + 1, d_out), 5.0, dtype=side.types[yt], device="cuda")
+        codes, sc, of = side.dev(packed), side.dev(scales), None if offs is None else side.dev(offs)
+        M = bf.bf_q4_matrix.of(codes, sc, of, d_in, group)
+        bf.bf_q4_linear(side.t, M, bf.bf_rows.of(x), n, bf.bf_rows.of(y))
+        got, xd = side.host(y), side.host(x)
+        want = xd @ W.T
+        off = np.abs(got[:n] - want) - linear_tolerance(xd, want, top, yt)
+        assert (off <= 0).all(), (xt, yt, offsets, off.max())
+        assert (got[n:] == 5).all()
+    bf.bf_trusted_status(side.t)
+
+
+@gpu
+@pytest.mark.parametrize("n", [1, 5, 20])
+def test_linear_strided_and_unaligned_rows(side, n):
+    torch, rng = side.torch, np.random.default_rng(n)
+    for xt, yt in (("bf16", "fp32"), ("fp32", "fp16"), ("fp16", "bf16")):
+        packed, scales, _, W, top = draw_matrix(rng, 70, 333, 64, False)
+        codes, sc = side.dev(packed), side.dev(scales)
+        big = torch.randn((n, 3, 401), device="cuda").to(side.types[xt])
+        x = big[:, 1, 7:340]                                                        # odd stride, odd start
+        out = torch.full((n, 201), 5.0, device="cuda").to(side.types[yt])
+        y = out[:, 3:73]
+        bf.bf_q4_linear(side.t, bf.bf_q4_matrix.of(codes, sc, None, 333, 64), bf.bf_rows.of(x), n, bf.bf_rows.of(y))
+        xd, got = side.host(x), side.host(y)
+        want = xd @ W.T
+        assert (np.abs(got - want) <= linear_tolerance(xd, want, top, yt)).all()
+        assert (side.host(out[:, :3]) == 5).all() and (side.host(out[:, 73:]) == 5).all()
+
+
+@gpu
+def test_linear_extreme_values(side):
+    """Rows of zeros, of tiny and of huge values beside ordinary ones; a NaN or an infinity stays in its row."""
+    torch, rng = side.torch, np.random.default_rng(3)
+    packed, scales, offs, W, top = draw_matrix(rng, 48, 300, 32, True)
+    codes, sc, of = side.dev(packed), side.dev(scales), side.dev(offs)
+    M = bf.bf_q4_matrix.of(codes, sc, of, 300, 32)
+    x = torch.randn((6, 300), device="cuda")
+    x[0] = 0
+    x[1] *= 1e-30
+    x[2] *= 1e30
+    x[3, ::7] *= 1e5
+    for xt in ("fp32", "bf16"):
+        xx = x.to(side.types[xt])
+        xx[4, 100] = float("nan")
+        xx[5, 299] = float("inf")
+        y = torch.empty((6, 48), device="cuda")
+        bf.bf_q4_linear(side.t, M, bf.bf_rows.of(xx), 6, bf.bf_rows.of(y))
+        xd, got = side.host(xx[:4]), side.host(y)
+        want = xd @ W.T
+        assert (np.abs(got[:4] - want) <= linear_tolerance(xd, want, top, "fp32")).all()
+        assert (got[0] == 0).all() and not np.isfinite(got[4]).any() and not np.isfinite(got[5]).any()
+    h = torch.full((2, 300), 2.0 ** -24, device="cuda").half()                      # the smallest of the type
+    h[1] = 65504.0
+    y = torch.empty((2, 48), device="cuda")
+    bf.bf_q4_linear(side.t, M, bf.bf_rows.of(h), 2, bf.bf_rows.of(y))
+    xd, got = side.host(h), side.host(y)
+    want = xd @ W.T
+    assert (np.abs(got - want) <= linear_tolerance(xd, want, top, "fp32")).all()
+
+
+# ---- the cache
+
+class DeviceCache:
+    def __init__(self, side, c):
+        self.side, self.c = side, c
+        self.pool = side.dev(c.pool.reshape(c.layers, c.pages, c.heads, -1))
+        self.tables, self.lengths, self.refs = side.dev(c.tables), side.dev(c.lengths), side.dev(c.refs)
+        self.desc = bf.bf_kv4_cache.of(self.pool, self.tables, self.lengths, self.refs, c.D, c.G, c.T)
+
+    def same(self, pool=True):
+        h, c = self.side.host, self.c
+        assert np.array_equal(h(self.lengths), c.lengths)
+        assert np.array_equal(h(self.refs), c.refs)
+        assert np.array_equal(h(self.tables), c.tables)
+        if pool:
+            assert np.array_equal(h(self.pool).reshape(c.pool.shape), c.pool)
+
+
+def status_of(side):
+    try:
+        bf.bf_trusted_status(side.t)
+    except bf.BifrostError as e:
+        return e.code
+    return 0
+
+
+def fill(side, c, lens, seed=0, type="fp32"):
+    """A host cache with sequences of these lengths in all layers, its device twin, and nothing else in common with the kernels."""
+    rng = np.random.default_rng(seed)
+    order = rng.permutation(c.pages)
+    at = 0
+    for i, n in enumerate(lens):
+        need = -(-n // c.T)
+        c.tables[i, :need] = order[at:at + need]
+        c.refs[order[at:at + need]] = 1
+        at += need
+        c.lengths[i] = n
+        for layer in range(c.layers):
+            for t in range(n):
+                c.put(layer, i, t, rng.standard_normal((c.heads, c.D)) * 1.5, rng.standard_normal((c.heads, c.D)))
+    return DeviceCache(side, c)
+
+
+@gpu
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("type", ["bf16", "fp16", "fp32"])
+def test_append_bytes_and_read(side, D, G, type):
+    """Chunks of every raggedness, then single tokens: every byte of the pool is what the definition says, borders of codes
+    included; then read back, whole and in part."""
+    torch, T = side.torch, 32
+    c = ref.Cache(2, 14, 3, D, G, T, 4, 4, seed=D + G)
+    d = DeviceCache(side, c)
+    rng = np.random.default_rng(7)
+    for step, (seqs, counts) in enumerate([([2, 0, 3], [1, 40, 17]), ([0, 2, 3], [5, 15, 1]), ([1, 0, 2, 3], [64, 19, 16, 30]), ([3, 2], [1, 1])]):
+        bf.bf_kv4_grow(side.t, d.desc, side.ints(seqs), cs := side.ints(counts), len(seqs))
+        assert not c.grow(seqs, counts)
+        starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        for layer in range(2):
+            qkv = rng.standard_normal((int(starts[-1]) + 2, 7, D)) * rng.choice([0.01, 1, 30], (1, 7, 1))
+            qkv[0, :, :G] = np.arange(G) % 31 / 2                                    # many quotients exactly on a border
+            qkv[-3, :, -G:] = 3.25                                                   # a group of one value
+            qkv = torch.from_numpy(qkv).to(side.types[type]).cuda()
+            k, v = qkv[:, 1:4], qkv[:, 4:]
+            single = step == 3
+            bf.bf_kv4_append(side.t, d.desc, layer, sq := side.ints(seqs), None if single else (st := side.ints(starts)), len(seqs), max(counts), bf.bf_rows.of(k), bf.bf_rows.of(v))
+            kh, vh = side.host(k), side.host(v)
+            for i, a in enumerate(seqs):
+                for j in range(counts[i]):
+                    c.put(layer, a, int(c.lengths[a]) - counts[i] + j, kh[starts[i] + j], vh[starts[i] + j])
+            d.same()
+    assert status_of(side) == 0
+    for layer, first, counts in ((0, None, [3, 64, 1, 0]), (1, [60, 0, 31, 16], [4, 33, 2, 17])):
+        starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        k = torch.full((int(starts[-1]) + 1, 3, D), 9.0, device="cuda").to(side.types[type])
+        v = torch.full_like(k, 9.0)
+        st, fi = side.ints(starts), side.ints(first)
+        bf.bf_kv4_read(side.t, d.desc, layer, None, st, fi, 4, 64, bf.bf_rows.of(k), bf.bf_rows.of(v))
+        for x, held in zip((k, v), (0, 1)):
+            x = side.host(x)
+            assert (x[starts[-1]:] == 9).all()
+            for i in range(4):
+                n = int(c.lengths[i])
+                f = first[i] if first else n - counts[i]
+                want = c.get(layer, i, n)[held][f:f + counts[i]]
+                assert (np.abs(x[starts[i]:starts[i + 1]] - want) <= HALF_STEP[type] * np.abs(want) + 2.0 ** -24 * np.abs(want) + TINY[type]).all()
+    assert status_of(side) == 0
+
+
+@gpu
+def test_append_special_values(side):
+    torch = side.torch
+    c = ref.Cache(1, 4, 2, 64, 32, 16, 2, 2)
+    d = DeviceCache(side, c)
+    c.grow([0], [6])
+    bf.bf_kv4_grow(side.t, d.desc, side.ints([0]), n := side.ints([6]), 1)
+    x = np.random.default_rng(0).standard_normal((6, 2, 64)).astype(np.float32)
+    x[0, 0, 3] = np.nan
+    x[1, 0, :3] = [np.inf, -np.inf, 70000.0]
+    x[2] = 0
+    x[3] = 1e-9                                          # a scale that fp16 does not hold
+    x[3, :, 5] = -1e-9
+    x[4, 1] = 61440.0 * (-1.0) ** np.arange(64)
+    x[5] = 2.0 ** -14 * np.arange(64)
+    xs = side.dev(x)
+    st = side.ints([0, 6])
+    bf.bf_kv4_append(side.t, d.desc, 0, None, st, 1, 6, bf.bf_rows.of(xs), bf.bf_rows.of(xs))
+    for t in range(6):
+        c.put(0, 0, t, x[t].astype(np.float64), x[t].astype(np.float64))
+    got = side.host(d.pool).reshape(c.pool.shape)
+    # (which NaN a group has is not part of the definition)
+    gh, ch = (np.where(np.isnan(p.view(np.float16)), np.float16(np.nan), p.view(np.float16)).view(np.uint16) for p in (got.copy(), c.pool.copy()))
+    assert np.array_equal(gh, ch)
+    out = torch.zeros((6, 2, 64), device="cuda")
+    bf.bf_kv4_read(side.t, d.desc, 0, None, st, None, 1, 6, bf.bf_rows.of(out), bf.bf_rows.of(torch.empty_like(out)))
+    o = side.host(out)
+    assert np.isnan(o[0, 0, :32]).all() and np.isfinite(o[0, 0, 32:]).all() and np.isfinite(o[1:]).all() and (o[2] == 0).all()
+    assert status_of(side) == 0
+
+
+@gpu
+def test_append_and_read_leave_bad_calls_alone(side):
+    torch = side.torch
+    c = ref.Cache(1, 6, 1, 64, 64, 16, 3, 2)
+    c.grow([0, 1, 2], [20, 16, 1])
+    x = torch.randn((64, 1, 64), device="cuda")
+    for seqs, starts, code in (([0, 5], [0, 1, 2], bf.BF_ERR_RANGE), ([-1], [0, 1], bf.BF_ERR_RANGE), ([0], [0, 9], bf.BF_ERR_RANGE), ([2], [0, 2], bf.BF_ERR_RANGE),
+                               ([0], [3, 1], bf.BF_ERR_RANGE), ([0], [-2, 0], bf.BF_ERR_RANGE), ([1], [2, 2], 0)):
+        d = DeviceCache(side, c)
+        sq, st = side.ints(seqs), side.ints(starts)
+        only = [a for a, n in zip(seqs, np.diff(starts)) if 0 <= a < 3 and 0 < n <= 8 and n <= c.lengths[a]] if starts[0] >= 0 else []
+        before = side.host(d.pool).copy()
+        bf.bf_kv4_append(side.t, d.desc, 0, sq, st, len(seqs), 8, bf.bf_rows.of(x), bf.bf_rows.of(x))
+        assert status_of(side) == code
+        if not only:
+            assert np.array_equal(before, side.host(d.pool))
+        y = torch.full_like(x, 4.0)
+        bf.bf_kv4_read(side.t, d.desc, 0, sq, st, None, len(seqs), 8, bf.bf_rows.of(y), bf.bf_rows.of(torch.empty_like(y)))
+        assert status_of(side) == code
+        if not only:
+            assert (side.host(y) == 4).all()
+    # a sequence named twice is written once, as its first entry says; a page out of range and a length out of range are not followed
+    d = DeviceCache(side, c)
+    sq, st = side.ints([0, 0]), side.ints([0, 2, 4])
+    bf.bf_kv4_append(side.t, d.desc, 0, sq, st, 2, 2, bf.bf_rows.of(x), bf.bf_rows.of(x))
+    assert status_of(side) == bf.BF_ERR_RANGE
+    e = DeviceCache(side, c)
+    st1 = side.ints([0, 2])
+    bf.bf_kv4_append(side.t, e.desc, 0, None, st1, 1, 2, bf.bf_rows.of(x), bf.bf_rows.of(x))
+    assert np.array_equal(side.host(d.pool), side.host(e.pool)) and status_of(side) == 0
+    for page in (-1, 6, 2 ** 31 - 1):
+        d = DeviceCache(side, c)
+        d.tables[0, 1] = page
+        before = side.host(d.pool).copy()
+        bf.bf_kv4_append(side.t, d.desc, 0, None, st1, 1, 2, bf.bf_rows.of(x), bf.bf_rows.of(x))
+        assert status_of(side) == bf.BF_ERR_RANGE and np.array_equal(before, side.host(d.pool))
+    for length in (-1, 33, 2 ** 31 - 1):
+        d = DeviceCache(side, c)
+        d.lengths[0] = length
+        before = side.host(d.pool).copy()
+        bf.bf_kv4_append(side.t, d.desc, 0, None, st1, 1, 2, bf.bf_rows.of(x), bf.bf_rows.of(x))
+        assert status_of(side) == bf.BF_ERR_RANGE and np.array_equal(before, side.host(d.pool))
+
+
+def check_attention(side, d, layer, seqs, counts, q, heads, window, type, max_q=None, max_len=None, scale=None, starts_given=True):
+    torch, c = side.torch, d.c
+    starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    scale = c.D ** -0.5 if scale is None else scale
+    pad = torch.full((int(starts[-1]) + 3, heads + 1, c.D), 5.0, device="cuda").to(side.types[type])
+    out = pad[:, :heads]                                                            # rows and heads behind the last stay as they were
+    lse = torch.full((int(starts[-1]) + 1, heads), 5.0, device="cuda")
+    st, sq = side.ints(starts) if starts_given else None, side.ints(seqs)
+    bf.bf_kv4_attention(side.t, d.desc, layer, sq, st, len(counts), max_q or max(counts), max_len or max(1, int(c.lengths.max())), bf.bf_rows.of(q), heads,
+                        bf.bf_rows.of(out), scale, window, lse)
+    got, gl, qd = side.host(pad), side.host(lse), side.host(q)
+    assert (got[starts[-1]:] == 5).all() and (got[:, heads] == 5).all() and (gl[starts[-1]:] == 5).all()
+    for i, n in enumerate(counts):
+        a = seqs[i] if seqs is not None else i
+        want, wl, tol, tl = ref.attention(c, layer, a, qd[starts[i]:starts[i + 1]], scale, window)
+        g = got[starts[i]:starts[i + 1], :heads]
+        assert (np.abs(g - want) <= tol + HALF_STEP[type] * (np.abs(want) + tol) + TINY[type]).all(), (i, n, np.abs(g - want).max(), tol.max())
+        l = gl[starts[i]:starts[i + 1]]
+        assert np.array_equal(np.isneginf(l), np.isneginf(wl))
+        seen = ~np.isneginf(wl)
+        assert (np.abs(l[seen] - wl[seen]) <= tl[seen]).all()
+    return got
+
+
+@gpu
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 3), (4, 2), (7, 1), (16, 2), (9, 1), (40, 2), (66, 2)])
+def test_attention_against_64_bits(side, D, G, heads, kv_heads):
+    torch = side.torch
+    type = "bf16" if (D + G + heads) % 64 < 32 else "fp16"
+    c = ref.Cache(2, 40, kv_heads, D, G, 32, 6, 8, seed=heads)
+    lens = [1, 0, 33, 16, 100, 207]
+    d = fill(side, c, lens, seed=heads)
+    g = torch.Generator(device="cuda").manual_seed(heads)
+    for counts, window in (([1] * 6, 0), ([1] * 6, 20), ([1, 0, 5, 16, 17, 3], 0), ([3, 2, 33, 20, 1, 9], 18), ([1, 1, 1, 1, 70, 1], 0), ([1] * 6, 1)):
+        qkv = torch.randn((sum(counts), heads + 3, D), generator=g, device="cuda").to(side.types[type])
+        check_attention(side, d, 1, None, counts, qkv[:, 2:2 + heads], heads, window, type, starts_given=counts != [1] * 6)
+    assert status_of(side) == 0
+
+
+@gpu
+@pytest.mark.parametrize("T", [16, 48, 256])
+def test_attention_pages_lists_and_hints(side, T):
+    """Other pages, sequences named in any order and twice, bounds that are not tight, a hint of the length that is wrong."""
+    torch = side.torch
+    c = ref.Cache(1, 80, 2, 128, 64, T, 5, 20, seed=T)
+    d = fill(side, c, [300, 5, 257, 0, 1], seed=T)
+    q = torch.randn((40, 4, 128), device="cuda").half()
+    one = check_attention(side, d, 0, [2, 0, 2, 4], [3, 1, 3, 1], torch.cat([q[:3], q[3:4], q[:3], q[4:5]]), 4, 0, "fp16", max_q=9, max_len=1)
+    assert np.array_equal(one[:3], one[4:7])
+    check_attention(side, d, 0, [1, 0, 3], [1, 1, 1], q[:3], 4, 0, "fp16", max_len=100000, starts_given=False)
+    check_attention(side, d, 0, [0], [1], q[:1], 4, 7, "fp16", max_len=3)
+    assert status_of(side) == 0
+
+
+@gpu
+def test_attention_extreme_scores(side):
+    """Scores far apart, all alike, far below zero, and a growing row of them; a NaN in q stays in its row."""
+    torch = side.torch
+    c = ref.Cache(1, 40, 1, 64, 32, 16, 2, 40)
+    rng = np.random.default_rng(5)
+    c.grow([0], [600])
+    for t in range(600):
+        c.put(0, 0, t, np.full((1, 64), t / 8.0 - 40), rng.standard_normal((1, 64)) * (50 if t % 3 else 0.01))
+    d = DeviceCache(side, c)
+    q = torch.zeros((6, 2, 64), device="cuda")
+    q[0] = 0.02
+    q[1] = -0.02
+    q[2] = 5
+    q[3] = -5
+    q[4] = 0
+    q[5, 0] = 1e-6
+    q[5, 1] = 300
+    for type in ("fp16", "bf16"):
+        for j in range(6):
+            check_attention(side, d, 0, [0], [1], q[j:j + 1].to(side.types[type]), 2, 0, type)
+        check_attention(side, d, 0, [0], [6], q.to(side.types[type]), 2, 0, type)
+    q[1, 0, 3], q[2, 1, 5] = float("nan"), float("inf")
+    out = torch.zeros((6, 2, 64), device="cuda").half()
+    st = side.ints([0, 6])
+    bf.bf_kv4_attention(side.t, d.desc, 0, None, st, 1, 6, 600, qq := bf.bf_rows.of(qh := q.half()), 2, bf.bf_rows.of(out), 0.125, 0, None)
+    o = side.host(out)
+    assert np.isnan(o[1, 0]).all() and not np.isfinite(o[2, 1]).any()
+    keep = np.ones((6, 2), bool)
+    keep[1, 0] = keep[2, 1] = False
+    assert np.isfinite(o[keep]).all()
+    assert status_of(side) == 0
+
+
+@gpu
+def test_attention_leaves_bad_entries_alone(side):
+    torch = side.torch
+    c = ref.Cache(1, 8, 1, 64, 64, 16, 3, 3)
+    d0 = fill(side, c, [40, 20, 1])
+    q = torch.randn((6, 2, 64), device="cuda").half()
+    for seqs, starts, max_q in (([3], [0, 1], 1), ([-1], [0, 1], 1), ([0], [0, 3], 2), ([0], [2, 1], 2), ([0], [-1, 0], 1)):
+        out = torch.full((6, 2, 64), 3.0, device="cuda").half()
+        sq, st = side.ints(seqs), side.ints(starts)
+        bf.bf_kv4_attention(side.t, d0.desc, 0, sq, st, 1, max_q, 40, bf.bf_rows.of(q), 2, bf.bf_rows.of(out), 0.1, 0, None)
+        assert status_of(side) == bf.BF_ERR_RANGE and (side.host(out) == 3).all()
+    for length in (-3, 49, 2 ** 31 - 1):
+        d = DeviceCache(side, c)
+        d.lengths[0] = length
+        out = torch.full((6, 2, 64), 3.0, device="cuda").half()
+        bf.bf_kv4_attention(side.t, d.desc, 0, None, None, 1, 1, 40, bf.bf_rows.of(q), 2, bf.bf_rows.of(out), 0.1, 0, None)
+        assert status_of(side) == bf.BF_ERR_RANGE and (side.host(out) == 3).all()
+    # pages out of range are passed over: what is left is attended to
+    d = DeviceCache(side, c)
+    d.tables[0, 1] = 8
+    out = torch.zeros((1, 2, 64), device="cuda").half()
+    bf.bf_kv4_attention(side.t, d.desc, 0, None, None, 1, 1, 40, bf.bf_rows.of(q[:1]), 2, bf.bf_rows.of(out), 0.1, 0, None)
+    assert status_of(side) == bf.BF_ERR_RANGE
+    k, v = (x[np.r_[0:16, 32:40], 0] for x in c.get(0, 0, 40))
+    s = 0.1 * side.host(q[0]) @ k.T
+    p = np.exp(s - s.max(1, keepdims=True))
+    want = p / p.sum(1, keepdims=True) @ v
+    assert np.abs(side.host(out)[0] - want).max() <= 2.0 ** -9 * np.abs(v).max()
+
+
+# ---- pages
+
+@gpu
+@pytest.mark.parametrize("T,heads,layers", [(16, 1, 1), (32, 3, 2), (64, 8, 3)])
+def test_pages_through_a_life(side, T, heads, layers):
+    """Growing, forking, freeing and compacting at random, a page short now and then: tables, counts and bytes as the plain
+    lists have them."""
+    rng = np.random.default_rng(T)
+    c = ref.Cache(layers, 37, heads, 64, 32, T, 12, 6, seed=T)
+    c.pool[:] = rng.integers(0, 256, c.pool.shape)
+    d = DeviceCache(side, c)
+    codes = {"range": bf.BF_ERR_RANGE, "oom": bf.BF_ERR_OOM}
+    met = set()
+    for step in range(300):
+        what = rng.choice(["grow", "grow", "fork", "free", "compact"])
+        n = int(rng.integers(1, 7))
+        bad = set()
+        if what == "grow":
+            seqs, counts = rng.permutation(12)[:n].tolist(), rng.integers(0, 2 * T, n).tolist()
+            bad = c.grow(seqs, counts)
+            bf.bf_kv4_grow(side.t, d.desc, a := side.ints(seqs), b := side.ints(counts), n)
+        elif what == "fork":
+            src, dst = rng.integers(0, 6, n).tolist(), (6 + rng.permutation(6)[:n]).tolist()
+            bad = c.fork(src, dst)
+            bf.bf_kv4_fork(side.t, d.desc, a := side.ints(src), b := side.ints(dst), n)
+        elif what == "free":
+            seqs = rng.permutation(12)[:n].tolist()
+            c.free(seqs)
+            bf.bf_kv4_free(side.t, d.desc, a := side.ints(seqs), n)
+        else:
+            live = side.ints([-7])
+            bf.bf_kv4_compact(side.t, d.desc, None, None, live)
+            assert side.host(live)[0] == c.compact()
+        met |= {what, *bad}
+        assert status_of(side) == (codes["range"] if "range" in bad else codes["oom"] if bad else 0), (step, what)
+        d.same()
+    assert {"oom", "fork", "free", "compact", "grow"} <= met
+
+
+@gpu
+def test_pages_refuse_in_the_kernel(side):
+    c = ref.Cache(1, 6, 1, 64, 64, 16, 5, 3)
+    c.grow([0, 1], [20, 16])
+    R = bf.BF_ERR_RANGE
+
+    def run(call, *lists):
+        d = DeviceCache(side, c)
+        keep = [side.ints(x) for x in lists]
+        call(side.t, d.desc, *keep, len(lists[0]))
+        return d, status_of(side)
+
+    for seqs, counts in (([7], [1]), ([-1], [1]), ([0, 0], [1, 1]), ([0], [-1]), ([0], [29]), ([2], [49]), ([1], [2 ** 31 - 1])):
+        d, code = run(bf.bf_kv4_grow, seqs, counts)
+        assert code == R
+        if seqs == [0, 0]:
+            assert side.host(d.lengths)[0] == 21                                     # the first entry counts
+        else:
+            d.same()
+    for src, dst in (([7], [2]), ([0], [9]), ([0], [-1]), ([0], [1]), ([0], [0])):
+        d, code = run(bf.bf_kv4_fork, src, dst)
+        assert code == R
+        d.same()
+    d, code = run(bf.bf_kv4_fork, [0, 2], [2, 3])                                     # a branch of what becomes a branch in the same call
+    assert code == R and list(side.host(d.lengths)) == [20, 16, 20, 0, 0]
+    d, code = run(bf.bf_kv4_fork, [0, 1], [2, 2])
+    assert code == R and side.host(d.lengths)[2] == 20 and list(side.host(d.refs)[:3]) == [2, 1, 1]
+    d, code = run(bf.bf_kv4_free, [9])
+    assert code == R
+    d.same()
+    d, code = run(bf.bf_kv4_free, [0, 0, 0])                                          # freed once
+    assert code == 0 and list(side.host(d.refs)) == [0, 0, 1, 0, 0, 0] and list(side.host(d.lengths)) == [0, 16, 0, 0, 0]
+    d = DeviceCache(side, c)
+    d.refs[0] = 0                                                                    # a count that is wrong already does not go below zero
+    bf.bf_kv4_free(side.t, d.desc, a := side.ints([0]), 1)
+    assert status_of(side) == R and side.host(d.refs)[0] == 0
+    d = DeviceCache(side, c)
+    d.tables[0, 0], d.tables[1, 0] = 5, 77                                           # a free page, and none
+    bf.bf_kv4_compact(side.t, d.desc, None, None, None)
+    assert status_of(side) == R and side.host(d.tables)[0, 0] == -1 and side.host(d.tables)[1, 0] == -1
+
+
+@gpu
+def test_compact_into_other_arrays(side):
+    torch, rng = side.torch, np.random.default_rng(2)
+    c = ref.Cache(3, 3000, 2, 64, 64, 16, 40, 60)
+    c.pool[:] = rng.integers(0, 256, c.pool.shape)
+    c.grow(list(range(40)), rng.integers(1, 900, 40).tolist())
+    c.free(list(range(0, 40, 3)))
+    d = DeviceCache(side, c)
+    before = [side.host(x).copy() for x in (d.tables, d.refs)]
+    tables, refs, live = torch.full_like(d.tables, 9), torch.full_like(d.refs, 9), side.ints([0])
+    for _ in range(2):                                                               # the arrays of the cache stay, so it can be done again
+        bf.bf_kv4_compact(side.t, d.desc, tables, refs, live)
+    assert all(np.array_equal(side.host(x), y) for x, y in zip((d.tables, d.refs), before))
+    n = c.compact()
+    assert side.host(live)[0] == n and np.array_equal(side.host(tables), c.tables) and np.array_equal(side.host(refs), c.refs)
+    assert np.array_equal(side.host(d.pool).reshape(c.pool.shape), c.pool) and status_of(side) == 0
+
+
+# ---- together
+
+@gpu
+@pytest.mark.parametrize("D,G,T,type", [(64, 64, 16, "bf16"), (128, 32, 64, "fp16")])
+def test_a_decode_from_prompt_to_end(side, D, G, T, type):
+    """Prompts in, a few tokens each, a fork, more tokens, an end, a compaction, more tokens: every step's attention is right."""
+    torch, H, Hk, L = side.torch, 4, 2, 2
+    c = ref.Cache(L, 30, Hk, D, G, T, 6, 8)
+    d = DeviceCache(side, c)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def step(seqs, counts):
+        starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        sq, cs, st = side.ints(seqs), side.ints(counts), side.ints(starts)
+        bf.bf_kv4_grow(side.t, d.desc, sq, cs, len(seqs))
+        assert not c.grow(seqs, counts)
+        for layer in range(L):
+            qkv = torch.randn((sum(counts), H + 2 * Hk, D), generator=gen, device="cuda").to(side.types[type])
+            q, k, v = qkv.split([H, Hk, Hk], 1)
+            bf.bf_kv4_append(side.t, d.desc, layer, sq, st, len(seqs), max(counts), bf.bf_rows.of(k), bf.bf_rows.of(v))
+            kh, vh = side.host(k), side.host(v)
+            for i, a in enumerate(seqs):
+                for j in range(counts[i]):
+                    c.put(layer, a, int(c.lengths[a]) - counts[i] + j, kh[starts[i] + j], vh[starts[i] + j])
+            check_attention(side, d, layer, seqs, counts, q, H, 0, type)
+
+    step([0, 1, 2], [30, 7, 16])
+    for _ in range(3):
+        step([0, 1, 2], [1, 1, 1])
+    bf.bf_kv4_fork(side.t, d.desc, a := side.ints([0, 2, 0]), b := side.ints([3, 4, 5]), 3)
+    c.fork([0, 2, 0], [3, 4, 5])
+    step([5, 0, 3, 4, 2], [1, 2, 1, 3, 1])                                           # parents and branches go their ways
+    bf.bf_kv4_free(side.t, d.desc, e := side.ints([1, 0]), 2)
+    c.free([1, 0])
+    bf.bf_kv4_compact(side.t, d.desc)
+    c.compact()
+    step([2, 3, 4, 5], [1, 1, 1, 1])
+    d.same()
+    assert status_of(side) == 0
+
+
+@gpu
+def test_captured_step_replays_on_new_lengths(side):
+    """A captured step (pages, append, attention, projection) replayed: every replay is a token further, as eager steps are."""
+    torch, H, Hk, D = side.torch, 8, 2, 64
+    rng = np.random.default_rng(9)
+    packed, scales, _, _, _ = draw_matrix(rng, 100, H * D, 64, False)
+    codes, sc = side.dev(packed), side.dev(scales)
+    M = bf.bf_q4_matrix.of(codes, sc, None, H * D, 64)
+    qkv = torch.zeros((2, H + 2 * Hk, D), dtype=torch.bfloat16, device="cuda")
+    q, k, v = qkv.split([H, Hk, Hk], 1)
+    steps = [torch.randn(qkv.shape, device="cuda").bfloat16() for _ in range(40)]
+
+    def twin():
+        d = DeviceCache(side, ref.Cache(1, 12, Hk, D, 32, 16, 2, 6))
+        return d, torch.zeros((2, H, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 100), device="cuda")
+
+    def step(t, d, out, y):
+        bf.bf_kv4_grow(t, d.desc, None, None, 2)
+        bf.bf_kv4_append(t, d.desc, 0, None, None, 2, 1, bf.bf_rows.of(k), bf.bf_rows.of(v))
+        bf.bf_kv4_attention(t, d.desc, 0, None, None, 2, 1, 96, bf.bf_rows.of(q), H, bf.bf_rows.of(out), 0.125, 0, None)
+        bf.bf_q4_linear(t, M, bf.bf_rows.of(out.view(2, -1)), 2, bf.bf_rows.of(y))
+
+    eager, want = twin(), []
+    for x in steps:
+        qkv.copy_(x)
+        step(side.t, *eager)
+        want.append((side.host(eager[1]).copy(), side.host(eager[2]).copy()))
+    d, out, y = twin()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        # the context's own stream joins the capture by an event
+        capturing = torch.cuda.current_stream()
+        side.stream.wait_stream(capturing)
+        with torch.cuda.stream(side.stream):
+            step(side.t, d, out, y)
+            refused(bf.BF_ERR_INVALID_ARG, bf.bf_trusted_status, side.t)
+        capturing.wait_stream(side.stream)
+    for x, (a, b) in zip(steps, want):
+        qkv.copy_(x)
+        graph.replay()
+        assert np.array_equal(side.host(out), a) and np.array_equal(side.host(y), b)
+    assert status_of(side) == 0
+    assert np.array_equal(side.host(d.pool), side.host(eager[0].pool)) and side.host(d.lengths).tolist() == [40, 40]
+
+
+@gpu
+def test_two_contexts_on_two_streams(side):
+    """Calls of two contexts at the same time do not meet in a workspace."""
+    torch = side.torch
+    c = ref.Cache(1, 300, 1, 64, 64, 16, 2, 150)
+    d = fill(side, c, [2000, 1500])
+    other = torch.cuda.Stream()
+    t2 = bf.bf_trusted_create(1 << 20, other.cuda_stream)
+    qs = [torch.randn((2, 8, 64), device="cuda").half() for _ in range(2)]
+    torch.cuda.synchronize()
+
+    def call(t, q, out):
+        bf.bf_kv4_attention(t, d.desc, 0, None, None, 2, 1, 2000, bf.bf_rows.of(q), 8, bf.bf_rows.of(out), 0.125, 0, None)
+
+    want = [torch.empty_like(q) for q in qs]
+    for q, o in zip(qs, want):
+        call(side.t, q, o)
+    torch.cuda.synchronize()
+    outs = [[torch.zeros_like(q) for _ in range(50)] for q in qs]
+    torch.cuda.synchronize()
+    for i in range(50):
+        call(side.t, qs[0], outs[0][i])
+        call(t2, qs[1], outs[1][i])
+    torch.cuda.synchronize()
+    for got, w in zip(outs, want):
+        assert all(torch.equal(o, w) for o in got)
+    bf.bf_trusted_destroy(t2)
