@@ -12,29 +12,615 @@ struct Q4 {
     unsigned group_stride, d_out, d_in, group;
 };
 
-constexpr unsigned WARPS = 8;
+// Codes go into the matrix instruction as they are.  A nibble at bits 0..3 or 4..7 of a 16-bit half IS an fp16 number, code * 2^-24 or
+// code * 2^-20 (both below the normal range, both exact), so that one AND makes two operands, against three instructions
+// for a conversion: 5 per 8 codes.  x carries the 2^-4 that the second kind is too large by.  Products of 11-bit x and 4-bit codes are
+// exact, sums are fp32; the 8 that a code is offset by enters as the accumulator's start, -8 sum x, and the scale of a
+// group multiplies the 32 to 128 columns' sum in fp32.
+//
+// x is held as fp16 relative to the largest of 256 columns (2^14 .. 2^15), which loses nothing of bf16 or fp16 above
+// 2^-24 of that; fp32 takes two columns of the instruction, x = hi + 2^-11 lo.
+constexpr unsigned SEG = 256, SEG_BLOCKS = SEG / 32;          // columns of a stage; blocks of 32 columns in it
+constexpr unsigned CODE_BYTES = 16 * SEG / 2;                 // 16 rows of a stage
 
-// One warp a row of W and row of x: sum_g s_g sum_c x_c (code_c - 8) + z_g sum_c x_c, in fp32.
-__global__ void __launch_bounds__(WARPS * 32) q4_linear_kernel(Q4 w, bf_rows x, unsigned n, bf_rows y) {
-    const unsigned o = blockIdx.x * WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (o >= w.d_out) return;
-    for (unsigned i = blockIdx.y; i < n; i += gridDim.y) {
-        float sum = 0;
-        for (unsigned c0 = lane * 8; c0 < w.d_in; c0 += 256) {
-            const uint32_t word = *reinterpret_cast<const uint32_t*>(w.codes + o * w.row_bytes + c0 / 2);
-            const size_t g = (size_t)o * w.group_stride + c0 / w.group;
-            float a = 0, b = 0;
-            for (unsigned k = 0; k < 8 && c0 + k < w.d_in; ++k) {
-                const float v = load_as_float(x.data, x.type, (int64_t)i * x.row_stride + c0 + k);
-                a += v * (float)((int)(word >> (4 * k) & 15) - 8);
-                b += v;
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void copy16(uint32_t smem, const void* p) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p)); }
+__device__ __forceinline__ void copy16(uint32_t smem, const void* p, bool some) {       // zeros where not
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(p), "r"(some ? 16 : 0));
+}
+template <int BYTES> __device__ __forceinline__ void copy_par(uint32_t smem, const void* p) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(p));
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem), "l"(p), "n"(BYTES));
+}
+// four 8 x 16-byte tiles: lane l names row l % 8 of tile l / 8 and gets word l % 4 of row l / 4 of each
+__device__ __forceinline__ void load_words(uint32_t (&w)[4], uint32_t smem) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(smem) : "memory");
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+    __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// 256 columns of one row of x (a warp; 8 a lane), zero behind d_in
+__device__ __forceinline__ void x_load(float (&v)[8], const bf_rows& x, unsigned row, unsigned c0, unsigned d_in, bool wide) {
+    const unsigned c = c0 + 8 * (threadIdx.x & 31);
+    const int64_t at = (int64_t)row * x.row_stride + c;
+    if (wide && c + 8 <= d_in) {
+        if (x.type == BF_F32) {
+            const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x.data) + at);
+            const float4 a = p[0], b = p[1];
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x.data) + at);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (x.type == BF_BF16) {
+                    v[2 * i] = __uint_as_float(w[i] << 16);
+                    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                } else {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                    v[2 * i] = f.x;
+                    v[2 * i + 1] = f.y;
+                }
             }
-            sum += __half2float(w.scales[g]) * a;
-            if (w.offsets) sum += __half2float(w.offsets[g]) * b;
         }
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        if (lane == 0) store_from_float(y.data, y.type, (int64_t)i * y.row_stride + o, sum);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < d_in ? load_as_float(x.data, x.type, at + i) : 0.f;
     }
+}
+
+__device__ __forceinline__ float largest(const float (&v)[8], float big = 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(v[i]));
+    return big;
+}
+__device__ __forceinline__ float warp_largest(float big) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
+    return big;
+}
+
+// The same as operands, relative to `big`: a lane's 16 bytes at frag[(lane / 4 * cols + col) * 4 + lane % 4], the sums of the groups times
+// 2^-24 at sums[group * sums_step + col], and what undoes the scaling at undo[col] (from one lane where `tell`); fp32 fills two columns.
+template <int G>
+__device__ __forceinline__ void x_unit(float (&v)[8], float big, bool two, uint4* frag, float* sums, unsigned sums_step, float* undo, bool tell,
+                                       unsigned cols, unsigned col) {
+    const unsigned lane = threadIdx.x & 31;
+    // 2^k with 2^14 <= big 2^k < 2^15, where 2^k is a float
+    const int e = max(1, (int)(__float_as_uint(big) >> 23));
+    const float up = __uint_as_float((unsigned)min(253, 268 - e) << 23), down = __uint_as_float((unsigned)max(1, e - 14) << 23);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= up;
+    for (int part = 0; part < (two ? 2 : 1); ++part, ++col) {
+        __half h[8];
+        float s = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = __float2half_rn(v[i]);
+            s += __half2float(h[i]);
+        }
+        const float q = 0.0625f;
+        uint4 o;
+        o.x = half2_bits(__half2float(h[0]), __half2float(h[4]));
+        o.y = half2_bits(__half2float(h[1]) * q, __half2float(h[5]) * q);
+        o.z = half2_bits(__half2float(h[2]), __half2float(h[6]));
+        o.w = half2_bits(__half2float(h[3]) * q, __half2float(h[7]) * q);
+        frag[(lane / 4 * cols + col) * 4 + lane % 4] = o;
+#pragma unroll
+        for (int d = G / 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+        if (lane % (G / 8) == 0) sums[lane / (G / 8) * sums_step + col] = s * 0x1p-24f;
+        if (tell && lane == 0) undo[col] = part ? down * 0x1p-11f : down;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (v[i] - __half2float(h[i])) * 2048.f;
+    }
+}
+
+// Up to 8 columns of x that fit shared memory whole.  A warp takes 16 rows of W and every KW-th stage of 256 columns, brings the codes in by
+// asynchronous copies, STAGES - 1 ahead and without a barrier of the block, and multiplies them from there.
+constexpr unsigned STAGES = 4, X_AT_ONCE = 4, MOST_WARPS = 16;
+template <int G, bool OFFSETS> struct Stage { static constexpr unsigned BYTES = CODE_BYTES + 16 * (SEG / G) * 2 * (OFFSETS ? 2 : 1); };
+
+// the parameters that a row has in a stage: 2, 4 or 8 fp16 numbers
+template <int N> struct Pars {
+    uint32_t w[N / 2];
+    __device__ __forceinline__ void load(const void* p) {
+        if (N == 2) w[0] = *static_cast<const uint32_t*>(p);
+        if (N == 4) *reinterpret_cast<uint2*>(w) = *static_cast<const uint2*>(p);
+        if (N == 8) *reinterpret_cast<uint4*>(w) = *static_cast<const uint4*>(p);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        const __half2 h = *reinterpret_cast<const __half2*>(&w[i / 2]);
+        return i % 2 ? __high2float(h) : __low2float(h);
+    }
+};
+
+template <int G, bool OFFSETS>
+__global__ void __launch_bounds__(MOST_WARPS * 32) q4_few_kernel(Q4 w, bf_rows x, unsigned n, bf_rows y, unsigned cols, unsigned kw, bool wide) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    constexpr unsigned STAGE = Stage<G, OFFSETS>::BYTES, GROUPS = SEG / G, PAR = GROUPS * 2;
+    const unsigned warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, j = lane % 4;
+    const unsigned segs = (w.d_in + SEG - 1) / SEG, per_block = warps / kw, mine = warp / kw, k0 = warp % kw;
+    const unsigned tiles = (w.d_out + 15) / 16, rounds = (tiles + gridDim.x * per_block - 1) / (gridDim.x * per_block);
+    unsigned char* ring = smem + warp * (STAGES * STAGE);
+    uint4* frag = reinterpret_cast<uint4*>(smem + warps * (STAGES * STAGE));
+    float* sums = reinterpret_cast<float*>(frag + (size_t)segs * SEG_BLOCKS * cols * 4);
+    float* undo = sums + segs * GROUPS * 8;
+    float* red = undo + segs * 8;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const unsigned per_tile = k0 < segs ? (segs - k0 + kw - 1) / kw : 0;       // stages of a tile that are this warp's
+
+    // the sequence of stages: tiles of this warp, in each its stages.  A lane copies 16 bytes of row lane / 8 and of the rows 4, 8, 12 below;
+    // block b of row r lies at 128 r + 16 (b ^ r % 8): a row's copies fill one line, and eight rows are read without conflicts
+    unsigned in_tile = mine * gridDim.x + blockIdx.x, in_seg = k0, in_slot = 0;
+    const unsigned cr = lane / 8, cb = lane % 8;
+    const uint32_t to_lo = ring_at + cr * 128 + ((cr ^ cb) * 16), to_hi = ring_at + (cr + 4) * 128 + (((cr + 4) ^ cb) * 16);
+    const uint32_t to_par = ring_at + CODE_BYTES + lane * PAR;
+    const size_t four_rows = 4 * w.row_bytes;
+    const uint8_t* from = nullptr;
+    const __half* from_par = nullptr;
+    auto at_tile = [&]() {
+        from = w.codes + (size_t)(in_tile * 16 + cr) * w.row_bytes + cb * 16 + (size_t)in_seg * (SEG / 2);
+        const unsigned o = min(in_tile * 16 + lane % 16, w.d_out - 1);
+        from_par = (OFFSETS && lane >= 16 ? w.offsets : w.scales) + (size_t)o * w.group_stride + in_seg * GROUPS;
+    };
+    at_tile();
+    auto fetch = [&]() {
+        if (in_tile < tiles && per_tile) {
+            const uint32_t slot_at = in_slot * STAGE;
+            if (in_tile * 16 + 16 <= w.d_out && (size_t)(in_seg + 1) * (SEG / 2) <= w.row_bytes) {
+                copy16(to_lo + slot_at, from);
+                copy16(to_hi + slot_at, from + four_rows);
+                copy16(to_lo + slot_at + 1024, from + 2 * four_rows);
+                copy16(to_hi + slot_at + 1024, from + 3 * four_rows);
+            } else {                                             // rows behind the last and bytes behind a row's: zeros
+                const bool in_row = (size_t)in_seg * (SEG / 2) + cb * 16 < w.row_bytes;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool some = in_row && in_tile * 16 + cr + 4 * i < w.d_out;
+                    copy16((i % 2 ? to_hi : to_lo) + slot_at + i / 2 * 1024, some ? from + i * four_rows : w.codes, some);
+                }
+            }
+            if (OFFSETS || lane < 16) copy_par<PAR>(to_par + slot_at, from_par);
+            in_slot = in_slot + 1 == STAGES ? 0 : in_slot + 1;
+            in_seg += kw;
+            from += kw * (SEG / 2);
+            from_par += kw * GROUPS;
+            if (in_seg >= segs) {
+                in_seg = k0;
+                in_tile += gridDim.x * per_block;
+                at_tile();
+            }
+        }
+        asm volatile("cp.async.commit_group;");
+    };
+#pragma unroll
+    for (unsigned i = 0; i + 1 < STAGES; ++i) fetch();
+
+    // (the rows of x come from L2 a few at a time: one after the other they would wait for it as often)
+    const bool two = x.type == BF_F32;
+    for (unsigned u0 = warp; u0 < segs * n; u0 += X_AT_ONCE * warps) {
+        float v[X_AT_ONCE][8];
+#pragma unroll
+        for (unsigned i = 0; i < X_AT_ONCE; ++i)
+            if (u0 + i * warps < segs * n) x_load(v[i], x, (u0 + i * warps) / segs, (u0 + i * warps) % segs * SEG, w.d_in, wide);
+#pragma unroll
+        for (unsigned i = 0; i < X_AT_ONCE; ++i) {
+            const unsigned seg = (u0 + i * warps) % segs, row = (u0 + i * warps) / segs;
+            if (u0 + i * warps < segs * n)
+                x_unit<G>(v[i], warp_largest(largest(v[i])), two, frag + (size_t)seg * SEG_BLOCKS * cols * 4, sums + seg * GROUPS * 8, 8, undo + seg * 8,
+                          true, cols, two ? 2 * row : row);
+        }
+    }
+    __syncthreads();
+
+    // (columns of the instruction behind the last of x repeat one; nobody reads their sums)
+    const uint4* my_frag = frag + min(g, cols - 1) * 4 + j;
+    const unsigned fr_step = cols * 4;
+    uint32_t rows_at[SEG_BLOCKS / 2];                            // this lane's row of the two blocks 2 p, 2 p + 1, for load_words
+#pragma unroll
+    for (unsigned p = 0; p < SEG_BLOCKS / 2; ++p) {
+        const unsigned b = 2 * p + lane / 16, row = lane % 16;
+        rows_at[p] = row * 128 + ((b ^ row % 8) * 16);
+    }
+    unsigned slot = 0;
+    for (unsigned r = 0; r < rounds; ++r) {
+        const unsigned tile = (r * per_block + mine) * gridDim.x + blockIdx.x;   // (a last round in part falls to all blocks alike)
+        float total[4] = {};
+        if (tile < tiles)
+            for (unsigned seg = k0; seg < segs; seg += kw) {
+                fetch();
+                asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1));
+                __syncwarp();
+                const unsigned char* st = ring + slot * STAGE;
+                const uint4* fr = my_frag + (size_t)seg * SEG_BLOCKS * cols * 4;
+                const float* xs_at = sums + seg * GROUPS * 8 + 2 * j;
+                const unsigned groups = (w.d_in - seg * SEG + G - 1) / G;      // (x is zero behind d_in, a scale may be anything)
+                Pars<GROUPS> s0, s1, z0, z1;
+                s0.load(st + CODE_BYTES + g * PAR);
+                s1.load(st + CODE_BYTES + (g + 8) * PAR);
+                if (OFFSETS) {
+                    z0.load(st + CODE_BYTES + (g + 16) * PAR);
+                    z1.load(st + CODE_BYTES + (g + 24) * PAR);
+                }
+                float part[4] = {};
+                const uint32_t stage_at = ring_at + slot * STAGE;
+#pragma unroll
+                for (int e = 0; e < (int)GROUPS; ++e) {
+                    const float2 xs = *reinterpret_cast<const float2*>(xs_at + e * 8);
+                    float acc[4] = {-8.f * xs.x, -8.f * xs.y, -8.f * xs.x, -8.f * xs.y}, acc2[4] = {};
+                    uint32_t word[4];                            // of rows g, g + 8 in an even block, and in the one behind it
+#pragma unroll
+                    for (int bb = 0; bb < G / 32; ++bb) {
+                        const int b = e * (G / 32) + bb;
+                        if (b % 2 == 0 || bb == 0) load_words(word, stage_at + rows_at[b / 2]);
+                        const uint32_t w0 = word[b % 2 * 2], w1 = word[b % 2 * 2 + 1];
+                        const uint4 f = fr[b * fr_step];
+                        const uint32_t a0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
+                        mma(acc, a0, f.x, f.y);
+                        const uint32_t v0 = w0 >> 8, v1 = w1 >> 8;
+                        const uint32_t a1[4] = {v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u};
+                        mma(acc2, a1, f.z, f.w);
+                    }
+                    const float f0 = e < (int)groups ? s0.get(e) : 0.f, f1 = e < (int)groups ? s1.get(e) : 0.f;
+                    part[0] += f0 * (acc[0] + acc2[0]), part[1] += f0 * (acc[1] + acc2[1]);
+                    part[2] += f1 * (acc[2] + acc2[2]), part[3] += f1 * (acc[3] + acc2[3]);
+                    if (OFFSETS) {
+                        const float h0 = e < (int)groups ? z0.get(e) : 0.f, h1 = e < (int)groups ? z1.get(e) : 0.f;
+                        part[0] += h0 * xs.x, part[1] += h0 * xs.y, part[2] += h1 * xs.x, part[3] += h1 * xs.y;
+                    }
+                }
+                const float2 un = *reinterpret_cast<const float2*>(undo + seg * 8 + 2 * j);
+                total[0] += un.x * part[0], total[1] += un.y * part[1], total[2] += un.x * part[2], total[3] += un.y * part[3];
+                __syncwarp();                                    // the slot is free for the next copy
+                slot = slot + 1 == STAGES ? 0 : slot + 1;
+            }
+        if (kw > 1) {                                            // the shares of a tile, in the order of the warps
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[warp * 128 + i * 32 + lane] = total[i];
+            __syncthreads();
+            if (k0 == 0)
+                for (unsigned k = 1; k < kw; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) total[i] += red[(warp + k) * 128 + i * 32 + lane];
+        }
+        if (tile < tiles && k0 == 0) {
+            const unsigned o = tile * 16 + g;
+            if (x.type == BF_F32) {
+                if (2 * j < cols) {
+                    if (o < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o, (total[0] + total[1]) * 0x1p24f);
+                    if (o + 8 < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o + 8, (total[2] + total[3]) * 0x1p24f);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned col = 2 * j + i % 2, row = o + i / 2 * 8;
+                    if (col < cols && row < w.d_out) store_from_float(y.data, y.type, (int64_t)col * y.row_stride + row, total[i] * 0x1p24f);
+                }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_all;");
+}
+
+constexpr unsigned SMEM_MAX = 227 * 1024;
+
+struct FewPlan { unsigned warps, kw, grid, smem; bool ok; };
+template <int G> FewPlan few_plan(const Q4& w, unsigned cols, unsigned n_sm) {
+    FewPlan p{};
+    const size_t segs = (w.d_in + SEG - 1) / SEG;
+    const size_t x_bytes = segs * SEG * 2 * cols + segs * (SEG / G) * 32 + segs * 32;
+    const unsigned tiles = (w.d_out + 15) / 16;
+    // warps along the columns: what leaves the longest-working warp the fewest stages, a round of joining counted as one
+    p.kw = 1;
+    size_t least = ~(size_t)0;
+    for (unsigned kw = 1; kw <= MOST_WARPS && (kw == 1 || kw / 2 < segs); kw *= 2) {
+        const size_t at_once = (size_t)n_sm * (MOST_WARPS / kw), cost = (tiles + at_once - 1) / at_once * ((segs + kw - 1) / kw + (kw > 1));
+        if (cost < least) least = cost, p.kw = kw;
+    }
+    // small matrices: blocks of as few warps as spread them over all SMs
+    p.warps = MOST_WARPS;
+    while (p.warps > p.kw && p.warps > 1 && (size_t)tiles * p.kw * 2 <= (size_t)n_sm * p.warps) p.warps /= 2;
+    const size_t bytes = x_bytes + p.warps * ((size_t)STAGES * (w.offsets ? Stage<G, true>::BYTES : Stage<G, false>::BYTES) + 512);
+    p.ok = bytes <= SMEM_MAX;
+    p.smem = (unsigned)bytes;
+    const unsigned per_block = p.warps / p.kw, blocks = (tiles + per_block - 1) / per_block;
+    p.grid = blocks < n_sm ? blocks : n_sm;
+    return p;
+}
+
+template <int G, bool OFFSETS> int few_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned n, const bf_rows& y, unsigned cols) {
+    const FewPlan p = few_plan<G>(w, cols, t->n_sm);
+    const cudaError_t e = cudaFuncSetAttribute(q4_few_kernel<G, OFFSETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
+    q4_few_kernel<G, OFFSETS><<<p.grid, p.warps * 32, p.smem, t->stream>>>(w, x, n, y, cols, p.kw, rows_wide(&x, false));
+    return launched(t, "q4_few_kernel");
+}
+
+// ------------------------------------------------------------------------------------------------
+// More columns, or more than shared memory holds.  x is laid out once, by a kernel of its own, and streamed with the weights.
+struct Prepared {
+    unsigned char* at;            // [column chunk][seg]: operands of `width` columns, then the sums of their groups
+    float* undo;                  // [columns]
+    unsigned width, segs;
+    size_t seg_bytes, chunk_bytes;
+};
+
+constexpr unsigned PREP_WARPS = 8;
+
+template <int G>
+__global__ void __launch_bounds__(PREP_WARPS * 32) q4_prepare_kernel(bf_rows x, unsigned row0, unsigned d_in, bool wide, Prepared p) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    __shared__ float most[PREP_WARPS];
+    const unsigned warp = threadIdx.x / 32, row = blockIdx.x;
+    const bool two = x.type == BF_F32;
+    float v[8], big = 0;
+    for (unsigned seg = warp; seg < p.segs; seg += PREP_WARPS) {
+        x_load(v, x, row0 + row, seg * SEG, d_in, wide);
+        big = largest(v, big);
+    }
+    big = warp_largest(big);
+    if (threadIdx.x % 32 == 0) most[warp] = big;
+    __syncthreads();
+#pragma unroll
+    for (unsigned i = 0; i < PREP_WARPS; ++i) big = fmaxf(big, most[i]);
+    const unsigned col = two ? 2 * row : row, chunk = col / p.width;          // (a chunk's width is even)
+    for (unsigned seg = warp; seg < p.segs; seg += PREP_WARPS) {
+        if (p.segs > PREP_WARPS) x_load(v, x, row0 + row, seg * SEG, d_in, wide);
+        unsigned char* at = p.at + chunk * p.chunk_bytes + seg * p.seg_bytes;
+        x_unit<G>(v, big, two, reinterpret_cast<uint4*>(at), reinterpret_cast<float*>(at + p.width * 512), p.width, p.undo + chunk * p.width, seg == 0,
+                  p.width, col % p.width);
+    }
+}
+
+// A block of 8 warps, kw of them along the columns; a warp has 32 rows of W, 8 NT columns.  All warps go through the stages together: a
+// stage holds kw times 256 columns of the rows and of x.
+constexpr unsigned MANY_WARPS = 8, ROWS = 32;
+template <int G, bool OFFSETS> struct Many {
+    static constexpr unsigned GROUPS = SEG / G, PAR = GROUPS * 2, CODES = ROWS * SEG / 2, WARP = CODES + ROWS * PAR * (OFFSETS ? 2 : 1);
+};
+
+template <int G, bool OFFSETS, int NT>
+__global__ void __launch_bounds__(MANY_WARPS * 32) q4_many_kernel(Q4 w, Prepared p, unsigned cols, unsigned kw, unsigned stages, bf_rows y, unsigned row0) {
+    using M = Many<G, OFFSETS>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    constexpr unsigned GROUPS = M::GROUPS, PAR = M::PAR, WIDTH = 8 * NT, X_SEG = WIDTH * 512 + GROUPS * WIDTH * 4;
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, j = lane % 4;
+    const unsigned per_block = MANY_WARPS / kw, mine = warp / kw, k0 = warp % kw;
+    const unsigned tiles = (w.d_out + ROWS - 1) / ROWS, steps = (p.segs + kw - 1) / kw;
+    const unsigned rounds = (tiles + gridDim.x * per_block - 1) / (gridDim.x * per_block);
+    const unsigned stage_bytes = MANY_WARPS * M::WARP + kw * X_SEG;
+    const uint32_t smem_at = (uint32_t)__cvta_generic_to_shared(smem);
+    float* red = reinterpret_cast<float*>(smem + stages * stage_bytes);
+    const unsigned char* x_from = p.at + blockIdx.y * p.chunk_bytes;
+
+    // the next stage to bring in
+    unsigned in_round = 0, in_step = 0, in_slot = 0;
+    const unsigned cr = lane / 8, cb = lane % 8;
+    auto fetch_weights = [&]() {
+        if (in_round >= rounds) return;
+        const unsigned tile = (in_round * per_block + mine) * gridDim.x + blockIdx.x, seg = in_step * kw + k0;
+        if (tile >= tiles || seg >= p.segs) return;
+        const uint32_t to = smem_at + in_slot * stage_bytes + warp * M::WARP;
+        const size_t at = (size_t)seg * (SEG / 2) + cb * 16;
+        const uint8_t* from = w.codes + (size_t)(tile * ROWS + cr) * w.row_bytes + at;
+        if (tile * ROWS + ROWS <= w.d_out && (size_t)(seg + 1) * (SEG / 2) <= w.row_bytes) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) copy16(to + (cr + 4 * i) * 128 + ((cb ^ ((cr + 4 * i) & 7)) * 16), from + (size_t)(4 * i) * w.row_bytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool some = at < w.row_bytes && tile * ROWS + cr + 4 * i < w.d_out;
+                copy16(to + (cr + 4 * i) * 128 + ((cb ^ ((cr + 4 * i) & 7)) * 16), some ? from + (size_t)(4 * i) * w.row_bytes : w.codes, some);
+            }
+        }
+        const size_t par = (size_t)min(tile * ROWS + lane, w.d_out - 1) * w.group_stride + seg * GROUPS;
+        copy_par<PAR>(to + M::CODES + lane * PAR, w.scales + par);
+        if (OFFSETS) copy_par<PAR>(to + M::CODES + (ROWS + lane) * PAR, w.offsets + par);
+    };
+    auto fetch_x = [&]() {
+        if (in_round < rounds) {
+            const unsigned segs = min(kw, p.segs - in_step * kw);
+            const uint32_t to = smem_at + in_slot * stage_bytes + MANY_WARPS * M::WARP;
+            const unsigned char* from = x_from + (size_t)in_step * kw * X_SEG;
+            for (unsigned o = threadIdx.x * 16; o < segs * X_SEG; o += MANY_WARPS * 32 * 16) copy16(to + o, from + o);
+        }
+        asm volatile("cp.async.commit_group;");
+        in_slot = in_slot + 1 == stages ? 0 : in_slot + 1;
+        if (++in_step == steps) in_step = 0, ++in_round;
+    };
+    // the first stages' weights do not wait for the kernel before this one, which writes x
+    for (unsigned i = 0; i + 1 < stages; ++i) {
+        fetch_weights();
+        in_slot = in_slot + 1 == stages ? 0 : in_slot + 1;
+        if (++in_step == steps) in_step = 0, ++in_round;
+    }
+    in_round = in_step = in_slot = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (unsigned i = 0; i + 1 < stages; ++i) fetch_x();
+
+    uint32_t rows_at[SEG_BLOCKS / 2];
+#pragma unroll
+    for (unsigned q = 0; q < SEG_BLOCKS / 2; ++q) rows_at[q] = lane % 16 * 128 + (((2 * q + lane / 16) ^ (lane & 7)) * 16);
+    unsigned slot = 0;
+    for (unsigned r = 0; r < rounds; ++r) {
+        const unsigned tile = (r * per_block + mine) * gridDim.x + blockIdx.x;
+        float total[2][NT][4] = {};
+        for (unsigned step = 0; step < steps; ++step) {
+            if (stages == 4) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            else if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                     // this stage is there, and all are done with the one before
+            fetch_weights();
+            fetch_x();
+            const unsigned seg = step * kw + k0;
+            if (tile < tiles && seg < p.segs) {
+                const unsigned char* st = smem + slot * stage_bytes + warp * M::WARP;
+                const uint32_t st_at = smem_at + slot * stage_bytes + warp * M::WARP;
+                const unsigned char* xs_seg = smem + slot * stage_bytes + MANY_WARPS * M::WARP + k0 * X_SEG;
+                const uint4* fr = reinterpret_cast<const uint4*>(xs_seg) + lane;
+                const float* sums = reinterpret_cast<const float*>(xs_seg + WIDTH * 512) + 2 * j;
+                const unsigned groups = (w.d_in - seg * SEG + G - 1) / G;      // (x is zero behind d_in, a scale may be anything)
+#pragma unroll
+                for (int e = 0; e < (int)GROUPS; ++e) {
+                    float acc[2][NT][4];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const float2 xs = *reinterpret_cast<const float2*>(sums + e * WIDTH + 8 * t);
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) acc[m][t][0] = acc[m][t][2] = -8.f * xs.x, acc[m][t][1] = acc[m][t][3] = -8.f * xs.y;
+                    }
+                    uint32_t word[2][4];
+#pragma unroll
+                    for (int bb = 0; bb < G / 32; ++bb) {
+                        const int b = e * (G / 32) + bb;
+                        if (b % 2 == 0 || bb == 0) {
+                            load_words(word[0], st_at + rows_at[b / 2]);
+                            load_words(word[1], st_at + 2048 + rows_at[b / 2]);
+                        }
+                        uint32_t a0[2][4], a1[2][4];
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const uint32_t w0 = word[m][b % 2 * 2], w1 = word[m][b % 2 * 2 + 1], v0 = w0 >> 8, v1 = w1 >> 8;
+                            a0[m][0] = w0 & 0x000f000fu, a0[m][1] = w1 & 0x000f000fu, a0[m][2] = w0 & 0x00f000f0u, a0[m][3] = w1 & 0x00f000f0u;
+                            a1[m][0] = v0 & 0x000f000fu, a1[m][1] = v1 & 0x000f000fu, a1[m][2] = v0 & 0x00f000f0u, a1[m][3] = v1 & 0x00f000f0u;
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const uint4 f = fr[(b * WIDTH + 8 * t) * 4];
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                mma(acc[m][t], a0[m], f.x, f.y);
+                                mma(acc[m][t], a1[m], f.z, f.w);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const __half* par = reinterpret_cast<const __half*>(st + M::CODES) + (16 * m + g) * GROUPS + e;
+                        const float f0 = e < (int)groups ? __half2float(par[0]) : 0.f, f1 = e < (int)groups ? __half2float(par[8 * GROUPS]) : 0.f;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            total[m][t][0] += f0 * acc[m][t][0], total[m][t][1] += f0 * acc[m][t][1];
+                            total[m][t][2] += f1 * acc[m][t][2], total[m][t][3] += f1 * acc[m][t][3];
+                        }
+                        if (OFFSETS) {
+                            const float h0 = e < (int)groups ? __half2float(par[ROWS * GROUPS]) : 0.f, h1 = e < (int)groups ? __half2float(par[(ROWS + 8) * GROUPS]) : 0.f;
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                const float2 xs = *reinterpret_cast<const float2*>(sums + e * WIDTH + 8 * t);
+                                total[m][t][0] += h0 * xs.x, total[m][t][1] += h0 * xs.y, total[m][t][2] += h1 * xs.x, total[m][t][3] += h1 * xs.y;
+                            }
+                        }
+                    }
+                }
+            }
+            slot = slot + 1 == stages ? 0 : slot + 1;
+        }
+        if (kw > 1) {                                            // the shares of a tile, in the order of the warps
+            __syncthreads();
+            float* to = red + warp * (2 * NT * 128) + lane;
+#pragma unroll
+            for (int i = 0; i < 2 * NT * 4; ++i) to[i * 32] = total[i / (4 * NT)][i / 4 % NT][i % 4];
+            __syncthreads();
+            if (k0 == 0)
+                for (unsigned k = 1; k < kw; ++k)
+#pragma unroll
+                    for (int i = 0; i < 2 * NT * 4; ++i) total[i / (4 * NT)][i / 4 % NT][i % 4] += to[k * (2 * NT * 128) + i * 32];
+        }
+        if (tile < tiles && k0 == 0) {
+            const bool two = cols >> 31;                         // (fp32: pairs of columns are one row of x)
+            const unsigned n_cols = cols & 0x7fffffffu;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const unsigned col = blockIdx.y * WIDTH + 8 * t + 2 * j;
+                if (col >= n_cols) continue;
+                const float u0 = p.undo[col], u1 = col + 1 < n_cols ? p.undo[col + 1] : 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                    // four rows of 16 m + 8 h + g
+                    const unsigned o = tile * ROWS + 8 * i + g;
+                    if (o >= w.d_out) continue;
+                    const float a = total[i / 2][t][i % 2 * 2] * u0, b = total[i / 2][t][i % 2 * 2 + 1] * u1;
+                    if (two) {
+                        store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, (a + b) * 0x1p24f);
+                    } else {
+                        store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, a * 0x1p24f);
+                        if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, b * 0x1p24f);
+                    }
+                }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_all;");
+}
+
+template <int G, bool OFFSETS, int NT>
+int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, unsigned rows, const bf_rows& y, Prepared p) {
+    using M = Many<G, OFFSETS>;
+    const bool two = x.type == BF_F32;
+    const unsigned cols = rows * (two ? 2 : 1), chunks = (cols + p.width - 1) / p.width, tiles = (w.d_out + ROWS - 1) / ROWS;
+    q4_prepare_kernel<G><<<rows, PREP_WARPS * 32, 0, t->stream>>>(x, row0, w.d_in, rows_wide(&x, false), p);
+    if (int rc = launched(t, "q4_prepare_kernel")) return rc;
+    // warps along the columns: what leaves the longest-working block the fewest steps, a round of joining counted as one; the x of a
+    // stage is at most 32 KB
+    unsigned kw = 1;
+    size_t least = ~(size_t)0;
+    for (unsigned k = 1; k <= MANY_WARPS && k * p.width <= 64 && (k == 1 || k / 2 < p.segs); k *= 2) {
+        const size_t at_once = (size_t)t->n_sm * (MANY_WARPS / k), cost = (tiles + at_once - 1) / at_once * ((p.segs + k - 1) / k + (k > 1));
+        if (cost < least) least = cost, kw = k;
+    }
+    const unsigned stage = MANY_WARPS * M::WARP + kw * (unsigned)p.seg_bytes, red = kw > 1 ? MANY_WARPS * 2 * NT * 512 : 0;
+    unsigned stages = 4;
+    while (stages > 2 && stages * stage + red > SMEM_MAX) --stages;
+    const unsigned per_block = MANY_WARPS / kw, blocks = (tiles + per_block - 1) / per_block;
+    cudaError_t e = cudaFuncSetAttribute(q4_many_kernel<G, OFFSETS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks < (unsigned)t->n_sm ? blocks : t->n_sm, chunks);
+    cfg.blockDim = MANY_WARPS * 32;
+    cfg.dynamicSmemBytes = stages * stage + red;
+    cfg.stream = t->stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, q4_many_kernel<G, OFFSETS, NT>, w, p, cols | (two ? 1u << 31 : 0), kw, stages, y, row0);
+    return e == cudaSuccess ? launched(t, "q4_many_kernel") : cuda_failed(t, "q4_many_kernel", e);
+}
+
+template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned n, const bf_rows& y) {
+    const unsigned per_row = x.type == BF_F32 ? 2 : 1, segs = (w.d_in + SEG - 1) / SEG;
+    // every block of the first kernel makes the operands of x itself
+    if ((uint64_t)n * per_row <= 8 && few_plan<G>(w, n * per_row, t->n_sm).ok) return few_launch<G, OFFSETS>(t, w, x, n, y, n * per_row);
+    // rows of x whose operands the workspace holds, in chunks of 8 to 64 columns; 65535 chunks at most
+    Prepared p{};
+    p.segs = segs;
+    const uint64_t all = (uint64_t)n * per_row;
+    p.width = all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : 64;
+    p.seg_bytes = p.width * (512 + SEG / G * 4);
+    p.chunk_bytes = p.seg_bytes * segs;
+    uint64_t chunks = t->ws_bytes / (p.chunk_bytes + p.width * 4 + 256);
+    if (chunks == 0) return BF_ERR_TOO_LARGE;
+    if (chunks > 1024) chunks = 1024;
+    const unsigned rows_at_once = (unsigned)(chunks * p.width / per_row);
+    for (unsigned r = 0; r < n; r += rows_at_once) {
+        const unsigned rows = n - r < rows_at_once ? n - r : rows_at_once;
+        p.undo = reinterpret_cast<float*>(t->ws);
+        p.at = t->ws + (((size_t)rows * per_row + p.width) * 4 + 255) / 256 * 256;
+        int rc = p.width == 8    ? many_launch<G, OFFSETS, 1>(t, w, x, r, rows, y, p)
+                 : p.width == 16 ? many_launch<G, OFFSETS, 2>(t, w, x, r, rows, y, p)
+                 : p.width == 32 ? many_launch<G, OFFSETS, 4>(t, w, x, r, rows, y, p)
+                                 : many_launch<G, OFFSETS, 8>(t, w, x, r, rows, y, p);
+        if (rc) return rc;
+    }
+    return BF_OK;
 }
 
 }  // namespace
@@ -50,6 +636,9 @@ extern "C" int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows*
     OnDevice on(t->device);
     if (!on.ok) return cuda_failed(t, "cudaSetDevice", cudaErrorInvalidDevice);
     const Q4 w{W->codes, (const __half*)W->scales, (const __half*)W->offsets, W->row_bytes, W->group_stride, W->d_out, W->d_in, W->group};
-    q4_linear_kernel<<<dim3((W->d_out + WARPS - 1) / WARPS, n < 65535 ? n : 65535), WARPS * 32, 0, t->stream>>>(w, *x, n, *y);
-    return launched(t, "q4_linear_kernel");
+    switch (W->group) {
+        case 32: return W->offsets ? linear<32, true>(t, w, *x, n, *y) : linear<32, false>(t, w, *x, n, *y);
+        case 64: return W->offsets ? linear<64, true>(t, w, *x, n, *y) : linear<64, false>(t, w, *x, n, *y);
+        default: return W->offsets ? linear<128, true>(t, w, *x, n, *y) : linear<128, false>(t, w, *x, n, *y);
+    }
 }
