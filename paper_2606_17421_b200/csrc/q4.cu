@@ -352,7 +352,8 @@ struct Prepared {
     size_t seg_bytes, chunk_bytes;
 };
 
-constexpr unsigned PREP_WARPS = 8;
+// One block a row of x: the largest of it, then its operands.  What the warps' first PREP_HELD segments read stays in registers.
+constexpr unsigned PREP_WARPS = 32, PREP_HELD = 2;
 
 template <int G>
 __global__ void __launch_bounds__(PREP_WARPS * 32) q4_prepare_kernel(bf_rows x, unsigned row0, unsigned d_in, bool wide, Prepared p) {
@@ -360,22 +361,33 @@ __global__ void __launch_bounds__(PREP_WARPS * 32) q4_prepare_kernel(bf_rows x, 
     __shared__ float most[PREP_WARPS];
     const unsigned warp = threadIdx.x / 32, row = blockIdx.x;
     const bool two = x.type == BF_F32;
-    float v[8], big = 0;
-    for (unsigned seg = warp; seg < p.segs; seg += PREP_WARPS) {
+    float held[PREP_HELD][8], v[8], big = 0;
+#pragma unroll
+    for (unsigned i = 0; i < PREP_HELD; ++i)
+        if (warp + i * PREP_WARPS < p.segs) x_load(held[i], x, row0 + row, (warp + i * PREP_WARPS) * SEG, d_in, wide);
+#pragma unroll
+    for (unsigned i = 0; i < PREP_HELD; ++i)
+        if (warp + i * PREP_WARPS < p.segs) big = largest(held[i], big);
+    for (unsigned seg = warp + PREP_HELD * PREP_WARPS; seg < p.segs; seg += PREP_WARPS) {
         x_load(v, x, row0 + row, seg * SEG, d_in, wide);
         big = largest(v, big);
     }
     big = warp_largest(big);
     if (threadIdx.x % 32 == 0) most[warp] = big;
     __syncthreads();
-#pragma unroll
-    for (unsigned i = 0; i < PREP_WARPS; ++i) big = fmaxf(big, most[i]);
+    big = warp_largest(most[threadIdx.x % 32]);
     const unsigned col = two ? 2 * row : row, chunk = col / p.width;          // (a chunk's width is even)
-    for (unsigned seg = warp; seg < p.segs; seg += PREP_WARPS) {
-        if (p.segs > PREP_WARPS) x_load(v, x, row0 + row, seg * SEG, d_in, wide);
+    auto make = [&](float (&u)[8], unsigned seg) {
         unsigned char* at = p.at + chunk * p.chunk_bytes + seg * p.seg_bytes;
-        x_unit<G>(v, big, two, reinterpret_cast<uint4*>(at), reinterpret_cast<float*>(at + p.width * 512), p.width, p.undo + chunk * p.width, seg == 0,
+        x_unit<G>(u, big, two, reinterpret_cast<uint4*>(at), reinterpret_cast<float*>(at + p.width * 512), p.width, p.undo + chunk * p.width, seg == 0,
                   p.width, col % p.width);
+    };
+#pragma unroll
+    for (unsigned i = 0; i < PREP_HELD; ++i)
+        if (warp + i * PREP_WARPS < p.segs) make(held[i], warp + i * PREP_WARPS);
+    for (unsigned seg = warp + PREP_HELD * PREP_WARPS; seg < p.segs; seg += PREP_WARPS) {
+        x_load(v, x, row0 + row, seg * SEG, d_in, wide);
+        make(v, seg);
     }
 }
 
@@ -387,7 +399,7 @@ template <int G, bool OFFSETS> struct Many {
 };
 
 template <int G, bool OFFSETS, int NT>
-__global__ void __launch_bounds__(MANY_WARPS * 32) q4_many_kernel(Q4 w, Prepared p, unsigned cols, unsigned kw, unsigned stages, bf_rows y, unsigned row0) {
+__global__ void __launch_bounds__(MANY_WARPS * 32, NT <= 4 ? 2 : 1) q4_many_kernel(Q4 w, Prepared p, unsigned cols, unsigned kw, unsigned stages, bf_rows y, unsigned row0) {
     using M = Many<G, OFFSETS>;
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr unsigned GROUPS = M::GROUPS, PAR = M::PAR, WIDTH = 8 * NT, X_SEG = WIDTH * 512 + GROUPS * WIDTH * 4;
@@ -491,15 +503,18 @@ __global__ void __launch_bounds__(MANY_WARPS * 32) q4_many_kernel(Q4 w, Prepared
                             a0[m][0] = w0 & 0x000f000fu, a0[m][1] = w1 & 0x000f000fu, a0[m][2] = w0 & 0x00f000f0u, a0[m][3] = w1 & 0x00f000f0u;
                             a1[m][0] = v0 & 0x000f000fu, a1[m][1] = v1 & 0x000f000fu, a1[m][2] = v0 & 0x00f000f0u, a1[m][3] = v1 & 0x00f000f0u;
                         }
+                        // (all of the first half, then all of the second: two that add to the same sums would wait for each other)
+                        uint4 f[NT];
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            const uint4 f = fr[(b * WIDTH + 8 * t) * 4];
+                        for (int t = 0; t < NT; ++t) f[t] = fr[(b * WIDTH + 8 * t) * 4];
 #pragma unroll
-                            for (int m = 0; m < 2; ++m) {
-                                mma(acc[m][t], a0[m], f.x, f.y);
-                                mma(acc[m][t], a1[m], f.z, f.w);
-                            }
-                        }
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) mma(acc[m][t], a0[m], f[t].x, f[t].y);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) mma(acc[m][t], a1[m], f[t].z, f[t].w);
                     }
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
@@ -567,22 +582,25 @@ int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
     const unsigned cols = rows * (two ? 2 : 1), chunks = (cols + p.width - 1) / p.width, tiles = (w.d_out + ROWS - 1) / ROWS;
     q4_prepare_kernel<G><<<rows, PREP_WARPS * 32, 0, t->stream>>>(x, row0, w.d_in, rows_wide(&x, false), p);
     if (int rc = launched(t, "q4_prepare_kernel")) return rc;
-    // warps along the columns: what leaves the longest-working block the fewest steps, a round of joining counted as one; the x of a
-    // stage is at most 32 KB
-    unsigned kw = 1;
+    // warps along the columns: what leaves the longest-working SM the fewest steps, a round of joining counted as one; the x of a
+    // stage is at most 32 KB.  Two blocks an SM where there is room and work for two.
+    unsigned kw = 1, per_sm = 1;
     size_t least = ~(size_t)0;
     for (unsigned k = 1; k <= MANY_WARPS && k * p.width <= 64 && (k == 1 || k / 2 < p.segs); k *= 2) {
-        const size_t at_once = (size_t)t->n_sm * (MANY_WARPS / k), cost = (tiles + at_once - 1) / at_once * ((p.segs + k - 1) / k + (k > 1));
-        if (cost < least) least = cost, kw = k;
+        const size_t bytes = 2 * (MANY_WARPS * M::WARP + k * p.seg_bytes) + (k > 1 ? MANY_WARPS * 2 * NT * 512 : 0);
+        const size_t blocks = (tiles + MANY_WARPS / k - 1) / (MANY_WARPS / k) * (size_t)chunks;
+        const unsigned two_fit = NT <= 4 && bytes <= SMEM_MAX / 2 - 1024 && blocks > (size_t)t->n_sm ? 2 : 1;
+        const size_t at_once = (size_t)t->n_sm * two_fit, cost = (blocks + at_once - 1) / at_once * ((p.segs + k - 1) / k + (k > 1)) * two_fit;
+        if (cost < least) least = cost, kw = k, per_sm = two_fit;
     }
     const unsigned stage = MANY_WARPS * M::WARP + kw * (unsigned)p.seg_bytes, red = kw > 1 ? MANY_WARPS * 2 * NT * 512 : 0;
     unsigned stages = 4;
-    while (stages > 2 && stages * stage + red > SMEM_MAX) --stages;
-    const unsigned per_block = MANY_WARPS / kw, blocks = (tiles + per_block - 1) / per_block;
+    while (stages > 2 && stages * stage + red > (per_sm == 2 ? SMEM_MAX / 2 - 1024 : SMEM_MAX)) --stages;
+    const unsigned per_block = MANY_WARPS / kw, blocks = (tiles + per_block - 1) / per_block, most_blocks = t->n_sm * per_sm;
     cudaError_t e = cudaFuncSetAttribute(q4_many_kernel<G, OFFSETS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
     if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks < (unsigned)t->n_sm ? blocks : t->n_sm, chunks);
+    cfg.gridDim = dim3(blocks < most_blocks ? blocks : most_blocks, chunks);
     cfg.blockDim = MANY_WARPS * 32;
     cfg.dynamicSmemBytes = stages * stage + red;
     cfg.stream = t->stream;
@@ -595,10 +613,13 @@ int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
     return e == cudaSuccess ? launched(t, "q4_many_kernel") : cuda_failed(t, "q4_many_kernel", e);
 }
 
+// Segments of x that every block makes operands of by itself; more are made once, which costs a launch.  4096 x 4096, 1 / 2 / 4 / 8 rows
+// (16 segments each): in every block 6.1 / 6.9 / 8.7 / 12.4 us, by a kernel of its own 6.7 / 6.7 / 6.7 / 6.7.
+constexpr unsigned FEW_UNITS = 32;
 template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned n, const bf_rows& y) {
     const unsigned per_row = x.type == BF_F32 ? 2 : 1, segs = (w.d_in + SEG - 1) / SEG;
     // every block of the first kernel makes the operands of x itself
-    if ((uint64_t)n * per_row <= 8 && few_plan<G>(w, n * per_row, t->n_sm).ok) return few_launch<G, OFFSETS>(t, w, x, n, y, n * per_row);
+    if ((uint64_t)n * per_row <= 8 && (uint64_t)n * segs <= FEW_UNITS && few_plan<G>(w, n * per_row, t->n_sm).ok) return few_launch<G, OFFSETS>(t, w, x, n, y, n * per_row);
     // rows of x whose operands the workspace holds, in chunks of 8 to 64 columns; 65535 chunks at most
     Prepared p{};
     p.segs = segs;
