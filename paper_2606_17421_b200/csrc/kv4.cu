@@ -183,57 +183,462 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
     }
 }
 
-// One block a (query head, row of a sequence, sequence); a warp takes a token at a time.
-template <int D, int G>
-__global__ void __launch_bounds__(128) attention_kernel(Cache c, unsigned layer, List l, bf_rows q, unsigned q_heads, bf_rows out, float scale,
-                                                        unsigned window, float* lse, int* status) {
+// ------------------------------------------------------------------------------------------------
+// Attention.  A block has the rows of one key head (its query heads, the tokens of a chunk) that fill NT columns of eight and a share of
+// the tokens; a warp takes every 8th sub-block of 16 tokens of that share, so that nothing but the end is shared in the block.
+//   S^T = K q^T: tokens x rows, codes as fp16 numbers below the normal range (code * 2^-24, or 2^-20 with q * 2^-4), so that an AND makes
+//         two operands; q relative to the largest of its row.  Per group of channels: score += scale_t * sum + low_t * (sum of q).
+//   softmax over tokens with a maximum per row that is only moved when a score exceeds it by 2^8: a vote a sub-block in the
+//         place of three exchanges.  p is held 2^6 up, so that fp16 takes what lies down to 2^-30 of the largest.
+//   O^T = V^T p: channels x rows, values (low + scale * code, one rounding) as the other operand; p^T by a transposition in registers.
+// Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
+// Bound by HBM for single tokens: 2.2 instructions a code at D = 128 against the 2.8 that the copy rate leaves time for.
+constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
+constexpr float P_SLACK = 8.f;
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ __half2 half2_of(uint32_t b) { return *reinterpret_cast<__half2*>(&b); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct Att {
+    Cache c;
+    List l;
+    bf_rows q, out;
+    const unsigned char* layer;    // of the pool
+    float* lse;
+    float* parts;                  // [block] rows x (D + 2) where a row's tokens are split
+    unsigned* arrivals;            // one for every set of splits
+    int* status;
+    unsigned per, q_heads, row_tiles, splits, window;
+    float scale;
+    int wide;
+};
+
+// Row r of a block's rows: its token's number in the sequence's rows, its query head
+struct Row {
+    int j, head;
+};
+
+template <int D, int G, int NT>
+__global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_kernel(const __grid_constant__ Att p) {
     using S = Sub<D, G>;
-    __shared__ float acc[4][D], stat[4][2];
-    const unsigned head = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kv = head / (q_heads / c.heads);
-    const int i = blockIdx.z, j = blockIdx.y;
-    const Span s = span_of(c, l, i);
+    constexpr int E = D / G, RW = 8 * NT, BLOCKS = D / 32, MT = D / 16;
+    constexpr bool HOLD = NT <= 2;                                           // operands of q in registers
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float sh_m[ATT_WARPS][RW], sh_l[ATT_WARPS][RW], row_scale[RW];
+    __shared__ unsigned last;
+    uint4* qf = reinterpret_cast<uint4*>(smem);                              // [BLOCKS][RW][4]
+    float* qs = reinterpret_cast<float*>(smem + BLOCKS * RW * 64);           // [E][RW] sums of q * 2^-24
+    unsigned char* ring = smem + BLOCKS * RW * 64 + E * RW * 4;              // [warp][stage][S::BYTES]; at the end [warp][8][D + 4] floats
+    const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, j4 = lane & 3;
+    unsigned block = blockIdx.x;
+    const unsigned split = block % p.splits;
+    block /= p.splits;
+    const unsigned set = block, tile = block % p.row_tiles;
+    block /= p.row_tiles;
+    const unsigned kv = block % p.c.heads, i = block / p.c.heads;
+    const Span s = span_of(p.c, p.l, i);
     if (!s.ok) {
-        if (threadIdx.x == 0 && s.rows != 0) atomicOr(status, ST_RANGE);
+        if (threadIdx.x == 0 && s.rows != 0) atomicOr(p.status, ST_RANGE);
         return;
     }
-    if (j >= s.rows) return;
-    const int pos = s.len - s.rows + j, first = window && pos >= (int)window ? pos - (int)window + 1 : 0;
-    const int64_t row = s.row0 + j;
-    float x[D / 32], o[D / 32] = {}, m = -CUDART_INF_F, sum = 0;
+    const int rows = s.rows * (int)p.per, r0 = (int)(tile * RW);
+    if (r0 >= rows) return;
+    // tokens that some row of this block sees, those that every row sees, and this block's share of the sub-blocks
+    const int before = s.len - s.rows;                                       // position of the sequence's first row
+    const int pos_first = before + r0 / (int)p.per, pos_last = before + (min(r0 + RW, rows) - 1) / (int)p.per;
+    const int win = p.window ? (int)min(p.window, 0x7fffffffu) : 0x7fffffff;
+    const int from = max(0, pos_first - win + 1), to = pos_last + 1, all_from = max(0, pos_last - win + 1), all_to = pos_first + 1;
+    const int sb0 = from / 16, n_sb = to > from ? (to + 15) / 16 - sb0 : 0, each = (n_sb + (int)p.splits - 1) / (int)p.splits;
+    const int sb_a = sb0 + min(n_sb, (int)split * each), sb_b = sb0 + min(n_sb, ((int)split + 1) * each);
+
+    // copies of this warp's sub-blocks.  Where they lie is looked up 32 at a time, by one lane each
+    const int mine = sb_b - sb_a > (int)warp ? (sb_b - sb_a - (int)warp + ATT_WARPS - 1) / ATT_WARPS : 0;
+    const int spp = p.c.page_tokens / 16;
+    const int* table = p.c.tables + (size_t)s.seq * p.c.max_pages;
+    unsigned char* my_ring = ring + warp * (ATT_STAGES * S::BYTES);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(my_ring) + lane * 16;
+    long long where = -1;
+    unsigned bad = 0;
+    int next = 0, next_slot = 0;
+    auto fetch = [&]() {
+        bad <<= 1;
+        if (next < mine) {
+            if (next % 32 == 0) {
+                where = -1;
+                if (next + (int)lane < mine) {
+                    const int sb = sb_a + (int)warp + ATT_WARPS * (next + (int)lane);
+                    const int page = table[sb / spp];
+                    if (page >= 0 && page < (int)p.c.n_pages)
+                        where = (long long)(((size_t)page * p.c.heads + kv) * p.c.block_bytes + (unsigned)(sb % spp) * S::BYTES);
+                    else atomicOr(p.status, ST_RANGE);
+                }
+            }
+            const long long at = __shfl_sync(~0u, where, next % 32);
+            if (at >= 0) {
+                const unsigned char* src = p.layer + at + lane * 16;
+                const uint32_t dst = ring_at + next_slot * S::BYTES;
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) x[e] = load_as_float(q.data, q.type, row * q.row_stride + head * q.head_stride + lane + 32 * e) * scale;
-    for (int t = first + warp; t <= pos; t += 4) {
-        const int page = c.tables[(size_t)s.seq * c.max_pages + t / c.page_tokens];
-        if (page < 0 || page >= (int)c.n_pages) {
-            if (lane == 0) atomicOr(status, ST_RANGE);
-            continue;
+                for (int o = 0; o < S::BYTES; o += 512)
+                    if (o + 512 <= S::BYTES || (int)lane * 16 < S::BYTES - o)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + o), "l"(src + o));
+            } else {
+                bad |= 1;
+            }
+            ++next;
+            next_slot = next_slot + 1 == ATT_STAGES ? 0 : next_slot + 1;
         }
-        const unsigned char* sub = c.pool + layer * c.layer_bytes + ((size_t)page * c.heads + kv) * c.block_bytes + (t % c.page_tokens) / 16 * S::BYTES;
-        float a = 0;
+        asm volatile("cp.async.commit_group;");
+    };
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) a += x[e] * key_at<D, G>(sub, t % 16, lane + 32 * e);
-        for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(~0u, a, d);
-        const float m2 = fmaxf(m, a), f = m == m2 ? 1.f : expf(m - m2), p = expf(a - m2);
-        sum = sum * f + p;
+    for (int k = 0; k < ATT_STAGES - 1; ++k) fetch();
+
+    // q of this block's rows as operands
+    for (int r = warp; r < RW; r += ATT_WARPS) {
+        const int rr = r0 + r;
+        float x[8] = {};
+        if (rr < rows && lane < D / 8) {
+            const int64_t at = (int64_t)(s.row0 + rr / (int)p.per) * p.q.row_stride + (int64_t)(kv * p.per + rr % p.per) * p.q.head_stride + 8 * lane;
+            if (p.wide) {
+                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q.data) + at);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = o[e] * f + p * value_at<D, G>(sub, t % 16, lane + 32 * e);
-        m = m2;
+                for (int k = 0; k < 4; ++k) {
+                    if (p.q.type == BF_BF16) {
+                        x[2 * k] = __uint_as_float(w[k] << 16);
+                        x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                    } else {
+                        const float2 f = __half22float2(half2_of(w[k]));
+                        x[2 * k] = f.x, x[2 * k + 1] = f.y;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = load_as_float(p.q.data, p.q.type, at + k);
+            }
+        }
+        float big = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[k]));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
+        // 2^k with 2^14 <= big 2^k < 2^15, where 2^k is a float
+        const int e = max(1, (int)(__float_as_uint(big) >> 23));
+        const float up = __uint_as_float((unsigned)min(253, 268 - e) << 23), down = __uint_as_float((unsigned)max(1, e - 14) << 23);
+        float h[8], sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            h[k] = __half2float(__float2half_rn(x[k] * up));
+            sum += h[k];
+        }
+        if (lane < D / 8) {
+            uint4 o;
+            o.x = bits(__floats2half2_rn(h[0], h[4]));
+            o.y = bits(__floats2half2_rn(h[1] * 0.0625f, h[5] * 0.0625f));
+            o.z = bits(__floats2half2_rn(h[2], h[6]));
+            o.w = bits(__floats2half2_rn(h[3] * 0.0625f, h[7] * 0.0625f));
+            qf[(lane / 4 * RW + r) * 4 + lane % 4] = o;
+        }
+#pragma unroll
+        for (int d = G / 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (lane < D / 8 && lane % (G / 8) == 0) qs[lane / (G / 8) * RW + r] = sum * 0x1p-24f;
+        if (lane == 0) row_scale[r] = p.scale * 1.4426950408889634f * (down * 0x1p24f);
     }
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) acc[warp][lane + 32 * e] = o[e];
-    stat[warp][0] = m;
-    stat[warp][1] = sum;
     __syncthreads();
-    float top = -CUDART_INF_F, all = 0, y = 0;
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w][0]);
-    for (int w = 0; w < 4; ++w) {
-        if (stat[w][1] == 0) continue;
-        const float f = expf(stat[w][0] - top);
-        all += f * stat[w][1];
-        if (threadIdx.x < D) y += f * acc[w][threadIdx.x];
+
+    uint4 held[HOLD ? BLOCKS : 1][HOLD ? NT : 1];
+    float held_sum[HOLD ? E : 1][HOLD ? NT : 1][2];
+    float coef[NT][2], m[NT][2], l[NT][2] = {}, o[MT][NT][4] = {};
+    int pos[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 8 * n + 2 * (int)j4 + h;
+            coef[n][h] = row_scale[r];
+            m[n][h] = -CUDART_INF_F;
+            pos[n][h] = r0 + r < rows ? before + (r0 + r) / (int)p.per : -1;
+        }
+        if (HOLD) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) held[b][n] = qf[(b * RW + 8 * n + g) * 4 + j4];
+#pragma unroll
+            for (int e = 0; e < E; ++e) held_sum[e][n][0] = qs[e * RW + 8 * n + 2 * j4], held_sum[e][n][1] = qs[e * RW + 8 * n + 2 * j4 + 1];
+        }
     }
-    if (threadIdx.x < D) store_from_float(out.data, out.type, row * out.row_stride + head * out.head_stride + threadIdx.x, all == 0 ? 0 : y / all);
-    if (lse && threadIdx.x == 0) lse[row * q_heads + head] = all == 0 ? -CUDART_INF_F : top + logf(all);
+
+    int slot = 0;
+    for (int it = 0; it < mine; ++it) {
+        fetch();
+        asm volatile("cp.async.wait_group %0;" ::"n"(ATT_STAGES - 1));
+        __syncwarp();
+        const unsigned char* sub = my_ring + slot * S::BYTES;
+        slot = slot + 1 == ATT_STAGES ? 0 : slot + 1;
+        if (bad >> (ATT_STAGES - 1) & 1) continue;
+        const int t0 = (sb_a + (int)warp + ATT_WARPS * it) * 16;
+        const bool masked = t0 < all_from || t0 + 16 > all_to;
+
+        // scores of tokens g, g + 8 and rows 2 j4, 2 j4 + 1
+        float x[NT][4] = {};
+        {
+            uint32_t word[BLOCKS][2];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; b += 2) {
+                const uint4 w = reinterpret_cast<const uint4*>(sub)[b * 16 + lane];
+                word[b][0] = w.x, word[b][1] = w.y, word[b + 1][0] = w.z, word[b + 1][1] = w.w;
+            }
+            uint32_t par[2][E];
+            {
+                const uint32_t* at = reinterpret_cast<const uint32_t*>(sub + S::K_PAR) + 2 * E * g;
+                if (E == 1) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(at);
+                    par[0][0] = v.x, par[1][0] = v.y;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2 * E; k += 4) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(at + k);
+                        par[k / E][k % E] = v.x, par[(k + 1) / E][(k + 1) % E] = v.y, par[(k + 2) / E][(k + 2) % E] = v.z, par[(k + 3) / E][(k + 3) % E] = v.w;
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float acc[NT][4] = {}, acc2[NT][4] = {};
+#pragma unroll
+                for (int bb = 0; bb < G / 32; ++bb) {
+                    const int b = e * (G / 32) + bb;
+                    const uint32_t w0 = word[b][0], w1 = word[b][1], v0 = w0 >> 8, v1 = w1 >> 8;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint4 f = HOLD ? held[HOLD ? b : 0][HOLD ? n : 0] : qf[(b * RW + 8 * n + g) * 4 + j4];
+                        mma(acc[n], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, f.x, f.y);
+                        mma(acc2[n], v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u, f.z, f.w);
+                    }
+                }
+                const float2 a = __half22float2(half2_of(par[0][e])), b = __half22float2(half2_of(par[1][e]));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float s0 = HOLD ? held_sum[HOLD ? e : 0][HOLD ? n : 0][0] : qs[e * RW + 8 * n + 2 * j4];
+                    const float s1 = HOLD ? held_sum[HOLD ? e : 0][HOLD ? n : 0][1] : qs[e * RW + 8 * n + 2 * j4 + 1];
+                    x[n][0] += a.x * (acc[n][0] + acc2[n][0]) + a.y * s0;
+                    x[n][1] += a.x * (acc[n][1] + acc2[n][1]) + a.y * s1;
+                    x[n][2] += b.x * (acc[n][2] + acc2[n][2]) + b.y * s0;
+                    x[n][3] += b.x * (acc[n][3] + acc2[n][3]) + b.y * s1;
+                }
+            }
+        }
+        bool over = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[n][k] *= coef[n][k % 2];
+                if (masked) {
+                    const int t = t0 + (int)g + k / 2 * 8;
+                    if (t > pos[n][k % 2] || t <= pos[n][k % 2] - win) x[n][k] = -CUDART_INF_F;
+                }
+                over |= x[n][k] > m[n][k % 2] + P_SLACK;
+            }
+        if (__any_sync(~0u, over)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float top = fmaxf(x[n][h], x[n][h + 2]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+                    top = fmaxf(top, m[n][h]);
+                    const float f = m[n][h] == top ? 1.f : exp2_fast(m[n][h] - top);
+                    m[n][h] = top;
+                    l[n][h] *= f;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) o[t][n][h] *= f, o[t][n][h + 2] *= f;
+                }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float base = m[n][h] == -CUDART_INF_F ? 0.f : m[n][h] - (float)P_UP;
+                x[n][h] = exp2_fast(x[n][h] - base);
+                x[n][h + 2] = exp2_fast(x[n][h + 2] - base);
+                l[n][h] += x[n][h] + x[n][h + 2];
+            }
+            pb[n][0] = transposed(bits(__floats2half2_rn(x[n][0], x[n][1])));
+            pb[n][1] = transposed(bits(__floats2half2_rn(x[n][2], x[n][3])));
+        }
+
+        // values of tokens 2 j4, 2 j4 + 1 and those 8 behind, channels g and g + 8 of 16
+        const __half2 k1024 = __floats2half2_rn(1024.f, 1024.f), k16 = __floats2half2_rn(0.0625f, 0.0625f), k64 = __floats2half2_rn(-64.f, -64.f);
+        uint4 par[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) par[e] = reinterpret_cast<const uint4*>(sub + S::V_PAR)[e * 4 + j4];
+        if (masked) {
+            // what no row sees may be anything.  A NaN that some rows see and others do not is taken out of the product, and given
+            // to the channels of those that do
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                uint32_t* w = reinterpret_cast<uint32_t*>(&par[e]);
+                unsigned odd = 0;                                            // which of the four tokens
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int t = t0 + 2 * (int)j4 + k % 2 + k / 2 * 8;
+                    const unsigned sh = 16 * (k % 2), sc = w[k / 2] >> sh & 0x7fff, lo = w[2 + k / 2] >> sh & 0x7fff;
+                    const bool seen = t >= from && t < to, off = sc >= 0x7c00 || lo >= 0x7c00;
+                    if (!seen || off) {
+                        w[k / 2] &= ~(0xffffu << sh);
+                        w[2 + k / 2] &= ~(0xffffu << sh);
+                    }
+                    if (seen && off) odd |= 1u << k;
+                }
+                if (__any_sync(~0u, odd))
+                    for (int u = 0; u < 16; ++u) {
+                        const unsigned theirs = __shfl_sync(~0u, odd, u / 2 % 4);
+                        if (!(theirs >> (u % 2 + u / 8 * 2) & 1)) continue;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                if (t0 + u <= pos[n][h] && t0 + u > pos[n][h] - win)
+#pragma unroll
+                                    for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t) o[t][n][h] = o[t][n][h + 2] = CUDART_NAN_F;
+                    }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            const uint4 w4 = reinterpret_cast<const uint4*>(sub + S::V_CODE)[c * 32 + lane];
+            const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int t = 4 * c + k, e = t * 16 / G;
+                const __half2 s01 = half2_of(par[e].x), s89 = half2_of(par[e].y), m01 = half2_of(par[e].z), m89 = half2_of(par[e].w);
+                const uint32_t w = word[k], v = w >> 8;
+                const __half2 c0 = __hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), k1024), c1 = __hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), k16, k64);
+                const __half2 c2 = __hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), k1024), c3 = __hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), k16, k64);
+                const uint32_t a0 = bits(__hfma2(c0, s01, m01)), a1 = bits(__hfma2(c1, s01, m01)), a2 = bits(__hfma2(c2, s89, m89)), a3 = bits(__hfma2(c3, s89, m89));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma(o[t][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+            }
+        }
+        __syncwarp();                                                        // the slot is free for the next copy
+    }
+    asm volatile("cp.async.wait_all;");
+
+    // the block's rows: maxima and sums of the warps, then their products, eight rows at a time where the copies were
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[n][h] += __shfl_xor_sync(~0u, l[n][h], d);
+            if (g == 0) {
+                sh_m[warp][8 * n + 2 * j4 + h] = m[n][h];
+                sh_l[warp][8 * n + 2 * j4 + h] = l[n][h];
+            }
+        }
+    float* red = reinterpret_cast<float*>(ring);
+    constexpr int PITCH = D + 4;
+    float* part = p.parts + (size_t)blockIdx.x * RW * (D + 2);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) red[(warp * 8 + 2 * j4 + k % 2) * PITCH + 16 * t + k / 2 * 8 + g] = o[t][n][k];
+        __syncthreads();
+        const int r = 8 * n + warp, rr = r0 + r;                             // a warp puts a row together
+        if (rr >= rows) continue;
+        float top = -CUDART_INF_F, sum = 0, y[D / 32] = {};
+#pragma unroll
+        for (int w = 0; w < ATT_WARPS; ++w) top = fmaxf(top, sh_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < ATT_WARPS; ++w) {
+            if (sh_l[w][r] == 0) continue;
+            const float f = sh_m[w][r] == top ? 1.f : exp2_fast(sh_m[w][r] - top);
+            sum += f * sh_l[w][r];
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) y[k] += f * red[(w * 8 + warp) * PITCH + lane + 32 * k];
+        }
+        if (p.splits == 1) {
+            const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
+            const float inv = sum == 0 ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + lane + 32 * k, y[k] * inv);
+            if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+        } else {
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) part[r * (D + 2) + lane + 32 * k] = y[k];
+            if (lane == 0) part[r * (D + 2) + D] = top, part[r * (D + 2) + D + 1] = sum;
+        }
+    }
+    if (p.splits == 1) return;
+    // the last block of a row's splits joins them, in their order
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(&p.arrivals[set], 1) == p.splits - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (threadIdx.x == 0) p.arrivals[set] = 0;
+    const float* first = p.parts + (size_t)(blockIdx.x - split) * RW * (D + 2);
+    for (int r = warp; r < RW && r0 + r < rows; r += ATT_WARPS) {
+        float top = -CUDART_INF_F, sum = 0, y[D / 32] = {};
+        for (unsigned k = 0; k < p.splits; ++k) top = fmaxf(top, __ldcg(first + ((size_t)k * RW + r) * (D + 2) + D));
+        for (unsigned k = 0; k < p.splits; ++k) {
+            const float* a = first + ((size_t)k * RW + r) * (D + 2);
+            const float ml = __ldcg(a + D), ll = __ldcg(a + D + 1);
+            if (ll == 0) continue;
+            const float f = ml == top ? 1.f : exp2_fast(ml - top);
+            sum += f * ll;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) y[c] += f * __ldcg(a + lane + 32 * c);
+        }
+        const int rr = r0 + r;
+        const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
+        const float inv = sum == 0 ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + lane + 32 * c, y[c] * inv);
+        if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+    }
+}
+
+template <int D, int G, int NT> int attention(bf_trusted* t, Att p, unsigned n, unsigned max_q, unsigned max_len) {
+    using S = Sub<D, G>;
+    constexpr unsigned RW = 8 * NT;
+    p.row_tiles = (unsigned)(((uint64_t)max_q * p.per + RW - 1) / RW);
+    const uint64_t sets = (uint64_t)n * p.c.heads * p.row_tiles;
+    if (sets >= (1u << 31) / 64) return BF_ERR_TOO_LARGE;
+    // tokens are split until there are blocks for two an SM, each with four sub-blocks a warp or more
+    const uint64_t seen = p.window && (uint64_t)p.window + max_q < max_len ? (uint64_t)p.window + max_q : max_len;
+    const uint64_t most = (seen + 16 * ATT_WARPS * 4 - 1) / (16 * ATT_WARPS * 4), wanted = (2 * (uint64_t)t->n_sm + sets - 1) / sets;
+    const uint64_t fit = t->ws_bytes / (sets * RW * (D + 2) * sizeof(float));
+    uint64_t splits = wanted < most ? wanted : most;
+    if (splits > fit) splits = fit;
+    if (splits < 1 || sets > ARRIVALS) splits = 1;
+    p.splits = (unsigned)splits;
+    constexpr size_t ring = (size_t)ATT_WARPS * ATT_STAGES * S::BYTES, red = (size_t)ATT_WARPS * 8 * (D + 4) * 4;
+    constexpr size_t smem = (D / 32) * RW * 64 + (D / G) * RW * 4 + (ring > red ? ring : red);
+    const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, G, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
+    attention_kernel<D, G, NT><<<(unsigned)(sets * splits), ATT_WARPS * 32, smem, t->stream>>>(p);
+    return launched(t, "attention_kernel");
 }
 
 template <typename F> void with_shape(const bf_kv4_cache* c, F f) {
@@ -295,12 +700,16 @@ extern "C" int bf_kv4_attention(bf_trusted* t, const bf_kv4_cache* c, uint32_t l
     if (int rc = io_check(t, c, &cache, layer, seqs, n, max_q, q, out)) return rc;
     if (q->type == BF_F32 || out->type != q->type || !max_len || !isfinite(scale)) return BF_ERR_INVALID_ARG;
     if (!n_q_heads || n_q_heads % c->n_kv_heads) return BF_ERR_SHAPE;
-    if (n > 65535 || max_q > 65535 || n_q_heads > 65535) return BF_ERR_TOO_LARGE;
     ON_DEVICE(t);
-    const List l{seqs, starts, n, max_q};
+    Att p{cache, List{seqs, starts, n, max_q}, *q, *out, cache.pool + layer * cache.layer_bytes, lse, (float*)t->ws, t->arrivals, t->status,
+          n_q_heads / c->n_kv_heads, n_q_heads, 0, 1, window, scale, rows_wide(q, true)};
+    const uint64_t rows = (uint64_t)max_q * p.per;
+    int rc = BF_OK;
     with_shape(c, [&](auto s) {
         using S = decltype(s);
-        attention_kernel<S::DIM, S::GROUP><<<dim3(n_q_heads, max_q, n), 128, 0, t->stream>>>(cache, layer, l, *q, n_q_heads, *out, scale, window, lse, t->status);
+        rc = rows <= 8 ? attention<S::DIM, S::GROUP, 1>(t, p, n, max_q, max_len)
+             : rows <= 16 ? attention<S::DIM, S::GROUP, 2>(t, p, n, max_q, max_len)
+                          : attention<S::DIM, S::GROUP, 4>(t, p, n, max_q, max_len);
     });
-    return launched(t, "attention_kernel");
+    return rc;
 }
