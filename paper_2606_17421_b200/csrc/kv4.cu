@@ -190,11 +190,13 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 //         two operands; q relative to the largest of its row.  Per group of channels: score += scale_t * sum + low_t * (sum of q).
 //   softmax over tokens with a maximum per row that is only moved when a score exceeds it by 2^8: a vote a sub-block in the
 //         place of three exchanges.  p is held 2^6 up, so that fp16 takes what lies down to 2^-30 of the largest.
-//   O^T = V^T p: channels x rows, values (low + scale * code, one rounding) as the other operand; p^T by a transposition in registers.
+//   O^T = V^T (p scale): channels x rows, codes taken the same way; p^T by a transposition in registers, times the scale of each
+//         token and group relative to a power of two that follows the largest.  The lows are a product of their own, a row a group.
 // Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
 // Bound by HBM for single tokens: 2.2 instructions a code at D = 128 against the 2.8 that the copy rate leaves time for.
 constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
-constexpr float P_SLACK = 8.f;
+constexpr float P_SLACK = 8.f, NO_BASE = 1e30f;
+constexpr unsigned MOST_SPLITS = 320;          // (their weights for 8 NT rows fit where the copies were)
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -233,11 +235,53 @@ struct Row {
     int j, head;
 };
 
+// Parameters of values where some row does not see some token.  What no row sees may be anything; a NaN that some rows see and others
+// do not is taken out of the product, and given to the channels of those that do.
+template <int D, int G, int NT>
+__device__ __forceinline__ void give_nan(unsigned odd, int e, float (&o)[D / 16][NT][4], int t0, const int (&pos)[NT][2], int win) {
+#pragma unroll 1
+    for (int u = 0; u < 16; ++u) {
+        const unsigned theirs = __shfl_sync(~0u, odd, u / 2 % 4);
+        if (!(theirs >> (u % 2 + u / 8 * 2) & 1)) continue;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (t0 + u <= pos[n][h] && t0 + u > pos[n][h] - win)
+#pragma unroll
+                    for (int t = 0; t < D / 16; ++t)
+                        if (t * 16 / G == e) o[t][n][h] = o[t][n][h + 2] = CUDART_NAN_F;
+    }
+}
+template <int D, int G, int NT>
+__device__ __forceinline__ void open_values(uint4 (&par)[D / G], float (&o)[D / 16][NT][4], int t0, int from, int to, const int (&pos)[NT][2], int win, int j4) {
+#pragma unroll
+    for (int e = 0; e < D / G; ++e) {
+        uint32_t w[4] = {par[e].x, par[e].y, par[e].z, par[e].w};
+        unsigned odd = 0;                                                    // which of the four tokens
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int t = t0 + 2 * j4 + k % 2 + k / 2 * 8;
+            const unsigned sh = 16 * (k % 2), sc = w[k / 2] >> sh & 0x7fff, lo = w[2 + k / 2] >> sh & 0x7fff;
+            const bool seen = t >= from && t < to, off = sc >= 0x7c00 || lo >= 0x7c00;
+            if (!seen || off) {
+                w[k / 2] &= ~(0xffffu << sh);
+                w[2 + k / 2] &= ~(0xffffu << sh);
+            }
+            if (seen && off) odd |= 1u << k;
+        }
+        par[e] = make_uint4(w[0], w[1], w[2], w[3]);
+        if (__any_sync(~0u, odd)) give_nan<D, G, NT>(odd, e, o, t0, pos, win);
+    }
+}
+
 template <int D, int G, int NT>
 __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_kernel(const __grid_constant__ Att p) {
     using S = Sub<D, G>;
     constexpr int E = D / G, RW = 8 * NT, BLOCKS = D / 32, MT = D / 16;
     constexpr bool HOLD = NT <= 2;                                           // operands of q in registers
+    // one column of rows: scales go to p, 5 instructions for 8 codes.  More: values are made once for all, 13 for 8.
+    constexpr bool SCALE_P = NT == 1;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ float sh_m[ATT_WARPS][RW], sh_l[ATT_WARPS][RW], row_scale[RW];
     __shared__ unsigned last;
@@ -272,25 +316,26 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     const int* table = p.c.tables + (size_t)s.seq * p.c.max_pages;
     unsigned char* my_ring = ring + warp * (ATT_STAGES * S::BYTES);
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(my_ring) + lane * 16;
-    long long where = -1;
-    unsigned bad = 0;
+    const unsigned char* my_layer = p.layer + lane * 16;
+    constexpr unsigned NOWHERE = 0xffffffffu;
+    unsigned where = NOWHERE, bad = 0;                                       // in the layer, in units of 16 bytes
     int next = 0, next_slot = 0;
     auto fetch = [&]() {
         bad <<= 1;
         if (next < mine) {
             if (next % 32 == 0) {
-                where = -1;
+                where = NOWHERE;
                 if (next + (int)lane < mine) {
                     const int sb = sb_a + (int)warp + ATT_WARPS * (next + (int)lane);
                     const int page = table[sb / spp];
                     if (page >= 0 && page < (int)p.c.n_pages)
-                        where = (long long)(((size_t)page * p.c.heads + kv) * p.c.block_bytes + (unsigned)(sb % spp) * S::BYTES);
+                        where = (unsigned)((((size_t)page * p.c.heads + kv) * p.c.block_bytes + (unsigned)(sb % spp) * S::BYTES) / 16);
                     else atomicOr(p.status, ST_RANGE);
                 }
             }
-            const long long at = __shfl_sync(~0u, where, next % 32);
-            if (at >= 0) {
-                const unsigned char* src = p.layer + at + lane * 16;
+            const unsigned at = __shfl_sync(~0u, where, next % 32);
+            if (at != NOWHERE) {
+                const unsigned char* src = my_layer + (size_t)at * 16;
                 const uint32_t dst = ring_at + next_slot * S::BYTES;
 #pragma unroll
                 for (int o = 0; o < S::BYTES; o += 512)
@@ -362,7 +407,11 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 
     uint4 held[HOLD ? BLOCKS : 1][HOLD ? NT : 1];
     float held_sum[HOLD ? E : 1][HOLD ? NT : 1][2];
-    float coef[NT][2], m[NT][2], l[NT][2] = {}, o[MT][NT][4] = {};
+    float coef[NT][2], base[NT][2], l[NT][2] = {}, o[MT][NT][4] = {};   // base: P_UP - the maximum that is held
+    float low[NT][4] = {};                                                   // of group g's lows
+    __half2 ref[E], inv_ref[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) ref[e] = __float2half2_rn(0.f), inv_ref[e] = __float2half2_rn(0.f);
     int pos[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -370,7 +419,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         for (int h = 0; h < 2; ++h) {
             const int r = 8 * n + 2 * (int)j4 + h;
             coef[n][h] = row_scale[r];
-            m[n][h] = -CUDART_INF_F;
+            base[n][h] = NO_BASE;
             pos[n][h] = r0 + r < rows ? before + (r0 + r) / (int)p.per : -1;
         }
         if (HOLD) {
@@ -426,7 +475,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                     for (int n = 0; n < NT; ++n) {
                         const uint4 f = HOLD ? held[HOLD ? b : 0][HOLD ? n : 0] : qf[(b * RW + 8 * n + g) * 4 + j4];
                         mma(acc[n], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, f.x, f.y);
-                        mma(acc2[n], v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u, f.z, f.w);
+                        mma(G == D ? acc2[n] : acc[n], v0 & 0x000f000fu, v1 & 0x000f000fu, v0 & 0x00f000f0u, v1 & 0x00f000f0u, f.z, f.w);
                     }
                 }
                 const float2 a = __half22float2(half2_of(par[0][e])), b = __half22float2(half2_of(par[1][e]));
@@ -434,91 +483,113 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                 for (int n = 0; n < NT; ++n) {
                     const float s0 = HOLD ? held_sum[HOLD ? e : 0][HOLD ? n : 0][0] : qs[e * RW + 8 * n + 2 * j4];
                     const float s1 = HOLD ? held_sum[HOLD ? e : 0][HOLD ? n : 0][1] : qs[e * RW + 8 * n + 2 * j4 + 1];
-                    x[n][0] += a.x * (acc[n][0] + acc2[n][0]) + a.y * s0;
-                    x[n][1] += a.x * (acc[n][1] + acc2[n][1]) + a.y * s1;
-                    x[n][2] += b.x * (acc[n][2] + acc2[n][2]) + b.y * s0;
-                    x[n][3] += b.x * (acc[n][3] + acc2[n][3]) + b.y * s1;
+#pragma unroll
+                    for (int k = 0; k < 4 && G == D; ++k) acc[n][k] += acc2[n][k];
+                    x[n][0] = fmaf(a.x, acc[n][0], fmaf(a.y, s0, x[n][0]));
+                    x[n][1] = fmaf(a.x, acc[n][1], fmaf(a.y, s1, x[n][1]));
+                    x[n][2] = fmaf(b.x, acc[n][2], fmaf(b.y, s0, x[n][2]));
+                    x[n][3] = fmaf(b.x, acc[n][3], fmaf(b.y, s1, x[n][3]));
                 }
             }
         }
-        bool over = false;
+        uint4 par[E];                                                        // of the values, for later
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < E; ++e) par[e] = reinterpret_cast<const uint4*>(sub + S::V_PAR)[e * 4 + j4];
+        if (masked) open_values<D, G, NT>(par, o, t0, from, to, pos, win, (int)j4);
+        bool over = false;
+        float y[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                x[n][k] *= coef[n][k % 2];
+                y[n][k] = fmaf(x[n][k], coef[n][k % 2], base[n][k % 2]);
                 if (masked) {
                     const int t = t0 + (int)g + k / 2 * 8;
-                    if (t > pos[n][k % 2] || t <= pos[n][k % 2] - win) x[n][k] = -CUDART_INF_F;
+                    if (t > pos[n][k % 2] || t <= pos[n][k % 2] - win) y[n][k] = -CUDART_INF_F;
                 }
-                over |= x[n][k] > m[n][k % 2] + P_SLACK;
             }
+            over |= fmaxf(y[n][0], y[n][2]) > P_UP + P_SLACK;
+            over |= fmaxf(y[n][1], y[n][3]) > P_UP + P_SLACK;
+        }
+        if (SCALE_P) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) over |= !__hbge2(ref[e], __hmax2(__habs2(half2_of(par[e].x)), __habs2(half2_of(par[e].y))));
+        }
         if (__any_sync(~0u, over)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float top = fmaxf(x[n][h], x[n][h + 2]);
+                    // (scores are masked where y is; what is not masked is not -inf in y unless it is in x)
+                    const float u = y[n][h] == -CUDART_INF_F ? y[n][h] : x[n][h] * coef[n][h], v = y[n][h + 2] == -CUDART_INF_F ? y[n][h + 2] : x[n][h + 2] * coef[n][h];
+                    float top = fmaxf(u, v);
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-                    top = fmaxf(top, m[n][h]);
-                    const float f = m[n][h] == top ? 1.f : exp2_fast(m[n][h] - top);
-                    m[n][h] = top;
-                    l[n][h] *= f;
+                    if (P_UP - top < base[n][h]) {
+                        const float f = base[n][h] == NO_BASE ? 0.f : exp2_fast(P_UP - top - base[n][h]);
+                        base[n][h] = P_UP - top;
+                        l[n][h] *= f;
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) o[t][n][h] *= f, o[t][n][h + 2] *= f;
+                        for (int t = 0; t < MT; ++t) o[t][n][h] *= f, o[t][n][h + 2] *= f;
+                        low[n][h] *= f;
+                        y[n][h] = u + base[n][h];
+                        y[n][h + 2] = v + base[n][h];
+                    }
                 }
+            if (SCALE_P) {
+                // scales are taken relative to a power of two that is at least the largest so far
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const __half2 h = __hmax2(__habs2(half2_of(par[e].x)), __habs2(half2_of(par[e].y)));
+                    float top = fmaxf(__low2float(h), __high2float(h));      // (passes over a NaN)
+#pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+                    const float old = __low2float(ref[e]);
+                    if (top > old) {
+                        // 2^15 at most, 2^-14 at least: ref and its inverse are both fp16 numbers
+                        const float now = top >= 32768.f ? 32768.f : fmaxf(__uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u), 0x1p-14f);
+                        const float f = old / now;
+                        ref[e] = __float2half2_rn(now);
+                        inv_ref[e] = __float2half2_rn(1.f / now);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) o[t][n][k] *= f;
+                    }
+                }
+            }
         }
         uint32_t pb[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float base = m[n][h] == -CUDART_INF_F ? 0.f : m[n][h] - (float)P_UP;
-                x[n][h] = exp2_fast(x[n][h] - base);
-                x[n][h + 2] = exp2_fast(x[n][h + 2] - base);
-                l[n][h] += x[n][h] + x[n][h + 2];
-            }
-            pb[n][0] = transposed(bits(__floats2half2_rn(x[n][0], x[n][1])));
-            pb[n][1] = transposed(bits(__floats2half2_rn(x[n][2], x[n][3])));
+            for (int k = 0; k < 4; ++k) y[n][k] = exp2_fast(y[n][k]);
+            l[n][0] += y[n][0] + y[n][2];
+            l[n][1] += y[n][1] + y[n][3];
+            pb[n][0] = transposed(bits(__floats2half2_rn(y[n][0], y[n][1])));
+            pb[n][1] = transposed(bits(__floats2half2_rn(y[n][2], y[n][3])));
         }
 
         // values of tokens 2 j4, 2 j4 + 1 and those 8 behind, channels g and g + 8 of 16
-        const __half2 k1024 = __floats2half2_rn(1024.f, 1024.f), k16 = __floats2half2_rn(0.0625f, 0.0625f), k64 = __floats2half2_rn(-64.f, -64.f);
-        uint4 par[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) par[e] = reinterpret_cast<const uint4*>(sub + S::V_PAR)[e * 4 + j4];
-        if (masked) {
-            // what no row sees may be anything.  A NaN that some rows see and others do not is taken out of the product, and given
-            // to the channels of those that do
+        uint32_t ps[SCALE_P ? E : 1][NT][2];
+        if (SCALE_P) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                uint32_t* w = reinterpret_cast<uint32_t*>(&par[e]);
-                unsigned odd = 0;                                            // which of the four tokens
+                const __half2 s01 = __hmul2(half2_of(par[e].x), inv_ref[e]), s89 = __hmul2(half2_of(par[e].y), inv_ref[e]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int t = t0 + 2 * (int)j4 + k % 2 + k / 2 * 8;
-                    const unsigned sh = 16 * (k % 2), sc = w[k / 2] >> sh & 0x7fff, lo = w[2 + k / 2] >> sh & 0x7fff;
-                    const bool seen = t >= from && t < to, off = sc >= 0x7c00 || lo >= 0x7c00;
-                    if (!seen || off) {
-                        w[k / 2] &= ~(0xffffu << sh);
-                        w[2 + k / 2] &= ~(0xffffu << sh);
-                    }
-                    if (seen && off) odd |= 1u << k;
+                for (int n = 0; n < NT; ++n) {
+                    ps[SCALE_P ? e : 0][n][0] = bits(__hmul2(half2_of(pb[n][0]), s01));
+                    ps[SCALE_P ? e : 0][n][1] = bits(__hmul2(half2_of(pb[n][1]), s89));
                 }
-                if (__any_sync(~0u, odd))
-                    for (int u = 0; u < 16; ++u) {
-                        const unsigned theirs = __shfl_sync(~0u, odd, u / 2 % 4);
-                        if (!(theirs >> (u % 2 + u / 8 * 2) & 1)) continue;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                if (t0 + u <= pos[n][h] && t0 + u > pos[n][h] - win)
-#pragma unroll
-                                    for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t) o[t][n][h] = o[t][n][h + 2] = CUDART_NAN_F;
-                    }
             }
+            uint32_t m01 = 0, m89 = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if ((int)g == e) m01 = par[e].z, m89 = par[e].w;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma(low[n], m01, 0u, m89, 0u, pb[n][0], pb[n][1]);
         }
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
@@ -527,19 +598,40 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int t = 4 * c + k, e = t * 16 / G;
-                const __half2 s01 = half2_of(par[e].x), s89 = half2_of(par[e].y), m01 = half2_of(par[e].z), m89 = half2_of(par[e].w);
                 const uint32_t w = word[k], v = w >> 8;
-                const __half2 c0 = __hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), k1024), c1 = __hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), k16, k64);
-                const __half2 c2 = __hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), k1024), c3 = __hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), k16, k64);
-                const uint32_t a0 = bits(__hfma2(c0, s01, m01)), a1 = bits(__hfma2(c1, s01, m01)), a2 = bits(__hfma2(c2, s89, m89)), a3 = bits(__hfma2(c3, s89, m89));
+                if (SCALE_P) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma(o[t][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                    for (int n = 0; n < NT; ++n)
+                        mma(o[t][n], w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u, ps[SCALE_P ? e : 0][n][0], ps[SCALE_P ? e : 0][n][1]);
+                } else {
+                    const __half2 k1024 = __floats2half2_rn(1024.f, 1024.f), k16 = __floats2half2_rn(0.0625f, 0.0625f), k64 = __floats2half2_rn(-64.f, -64.f);
+                    const __half2 s01 = half2_of(par[e].x), s89 = half2_of(par[e].y), m01 = half2_of(par[e].z), m89 = half2_of(par[e].w);
+                    const __half2 c0 = __hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), k1024), c1 = __hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), k16, k64);
+                    const __half2 c2 = __hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), k1024), c3 = __hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), k16, k64);
+                    const uint32_t a0 = bits(__hfma2(c0, s01, m01)), a1 = bits(__hfma2(c1, s01, m01)), a2 = bits(__hfma2(c2, s89, m89)), a3 = bits(__hfma2(c3, s89, m89));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma(o[t][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                }
             }
         }
         __syncwarp();                                                        // the slot is free for the next copy
     }
     asm volatile("cp.async.wait_all;");
 
+    if (SCALE_P)
+    // codes were taken as 2^-24 (channels g) and 2^-20 (g + 8) of themselves, scales relative to ref
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float f = __low2float(ref[e]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float add = __shfl_sync(~0u, low[n][h], 4 * e + j4);
+#pragma unroll
+                for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t) o[t][n][h] = o[t][n][h] * (f * 0x1p24f) + add, o[t][n][h + 2] = o[t][n][h + 2] * (f * 0x1p20f) + add;
+            }
+    }
     // the block's rows: maxima and sums of the warps, then their products, eight rows at a time where the copies were
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -548,7 +640,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l[n][h] += __shfl_xor_sync(~0u, l[n][h], d);
             if (g == 0) {
-                sh_m[warp][8 * n + 2 * j4 + h] = m[n][h];
+                sh_m[warp][8 * n + 2 * j4 + h] = base[n][h] == NO_BASE ? -CUDART_INF_F : (float)P_UP - base[n][h];
                 sh_l[warp][8 * n + 2 * j4 + h] = l[n][h];
             }
         }
@@ -598,24 +690,41 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     __threadfence();
     if (threadIdx.x == 0) p.arrivals[set] = 0;
     const float* first = p.parts + (size_t)(blockIdx.x - split) * RW * (D + 2);
-    for (int r = warp; r < RW && r0 + r < rows; r += ATT_WARPS) {
-        float top = -CUDART_INF_F, sum = 0, y[D / 32] = {};
-        for (unsigned k = 0; k < p.splits; ++k) top = fmaxf(top, __ldcg(first + ((size_t)k * RW + r) * (D + 2) + D));
-        for (unsigned k = 0; k < p.splits; ++k) {
-            const float* a = first + ((size_t)k * RW + r) * (D + 2);
-            const float ml = __ldcg(a + D), ll = __ldcg(a + D + 1);
-            if (ll == 0) continue;
-            const float f = ml == top ? 1.f : exp2_fast(ml - top);
-            sum += f * ll;
+    float* f_of = reinterpret_cast<float*>(smem);                            // [rows][splits] what a split's part counts for
+    const int n_rows = min(RW, rows - r0);
+    for (int r = warp; r < n_rows; r += ATT_WARPS) {
+        float top = -CUDART_INF_F, sum = 0;
+        for (unsigned k = lane; k < p.splits; k += 32) top = fmaxf(top, __ldcg(first + ((size_t)k * RW + r) * (D + 2) + D));
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) y[c] += f * __ldcg(a + lane + 32 * c);
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        for (unsigned k = lane; k < p.splits; k += 32) {
+            const float* a = first + ((size_t)k * RW + r) * (D + 2) + D;
+            const float ml = __ldcg(a), ll = __ldcg(a + 1), f = ll == 0 ? 0.f : ml == top ? 1.f : exp2_fast(ml - top);
+            f_of[r * p.splits + k] = f;
+            sum += ll == 0 ? 0.f : f * ll;
         }
-        const int rr = r0 + r;
-        const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
-        const float inv = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + lane + 32 * c, y[c] * inv);
-        if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        if (lane == 0) {
+            sh_l[0][r] = sum == 0 ? 0.f : 1.f / sum;
+            if (p.lse) {
+                const int64_t row = s.row0 + (r0 + r) / (int)p.per, head = kv * p.per + (r0 + r) % p.per;
+                p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+            }
+        }
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < n_rows * D; u += ATT_WARPS * 32) {
+        const int r = u / D, c = u % D, rr = r0 + r;
+        const float* a = first + (size_t)r * (D + 2) + c;
+        float y = 0;
+#pragma unroll 8
+        for (unsigned k = 0; k < p.splits; ++k) {
+            const float f = f_of[r * p.splits + k], v = __ldcg(a + (size_t)k * RW * (D + 2));
+            y += f == 0 ? 0.f : f * v;                                       // (a part that nothing was seen in holds zeros)
+        }
+        const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
+        store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + c, y * sh_l[0][r]);
     }
 }
 
@@ -630,6 +739,7 @@ template <int D, int G, int NT> int attention(bf_trusted* t, Att p, unsigned n, 
     const uint64_t most = (seen + 16 * ATT_WARPS * 4 - 1) / (16 * ATT_WARPS * 4), wanted = (2 * (uint64_t)t->n_sm + sets - 1) / sets;
     const uint64_t fit = t->ws_bytes / (sets * RW * (D + 2) * sizeof(float));
     uint64_t splits = wanted < most ? wanted : most;
+    if (splits > MOST_SPLITS) splits = MOST_SPLITS;
     if (splits > fit) splits = fit;
     if (splits < 1 || sets > ARRIVALS) splits = 1;
     p.splits = (unsigned)splits;

@@ -80,7 +80,7 @@ int bft::cache_check(const bf_kv4_cache* c, Cache* out) {
     if ((uint64_t)c->max_pages * c->page_tokens >= (1ull << 31) - 512 || c->n_pages >= (1u << 31) || c->n_seqs >= (1u << 31) ||
         c->n_kv_heads > 1024 || c->n_layers > (1u << 16) || (uint64_t)c->n_seqs * c->max_pages >= (1ull << 40)) return BF_ERR_SHAPE;
     const unsigned __int128 bytes = (unsigned __int128)c->n_pages * c->n_kv_heads * block * c->n_layers;
-    if (bytes >> 48) return BF_ERR_SHAPE;
+    if (bytes >> 48 || bytes / c->n_layers >= ((unsigned __int128)1 << 36)) return BF_ERR_SHAPE;    // (a layer's bytes / 16 are counted in 32 bits)
     out->pool = static_cast<unsigned char*>(c->pool);
     out->tables = c->tables;
     out->lengths = c->lengths;
