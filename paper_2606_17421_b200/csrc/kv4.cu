@@ -1,6 +1,9 @@
 // The cache in 4 bits: writing it, reading it back, and attention over it.
 #include <math_constants.h>
 
+#include <algorithm>
+
+
 #include "bf_trusted.h"
 
 using namespace bft;
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 // Bound by HBM for single tokens: 2.2 instructions a code at D = 128 against the 2.8 that the copy rate leaves time for.
 constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
 constexpr float P_SLACK = 8.f, NO_BASE = 1e30f;
-constexpr unsigned MOST_SPLITS = 320;          // (their weights for 8 NT rows fit where the copies were)
+constexpr unsigned PIECE = 128, MOST_SPLITS = 160;          // (what 8 NT rows of them count for fits where the copies were)
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -216,6 +219,20 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+// n / d by a multiplication where that is exact: m = 2^32 / d + 1 exceeds 2^32 / d by 1 at most, so that n m / 2^32 is off by less than
+// 1 / d while n d < 2^32
+struct Divisor {
+    unsigned d, m, below;
+    Divisor() = default;
+    explicit Divisor(unsigned by) : d(by), m(by > 1 ? (unsigned)((1ull << 32) / by + 1) : 0), below(by > 1 ? 0xffffffffu / by : 0) {}
+    __device__ __forceinline__ unsigned quotient(unsigned n) const { return n < below ? __umulhi(n, m) : d == 1 ? n : n / d; }
+    __device__ __forceinline__ unsigned split(unsigned n, unsigned& rest) const {
+        const unsigned q = quotient(n);
+        rest = n - q * d;
+        return q;
+    }
+};
+
 struct Att {
     Cache c;
     List l;
@@ -225,7 +242,9 @@ struct Att {
     float* parts;                  // [block] rows x (D + 2) where a row's tokens are split
     unsigned* arrivals;            // one for every set of splits
     int* status;
-    unsigned per, q_heads, row_tiles, splits, window;
+    Divisor per, row_tiles, splits, heads, spp;
+    unsigned q_heads, window;
+    int each;                      // sub-blocks of a split, where that is enough
     float scale;
     int wide;
 };
@@ -289,30 +308,58 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     float* qs = reinterpret_cast<float*>(smem + BLOCKS * RW * 64);           // [E][RW] sums of q * 2^-24
     unsigned char* ring = smem + BLOCKS * RW * 64 + E * RW * 4;              // [warp][stage][S::BYTES]; at the end [warp][8][D + 4] floats
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, j4 = lane & 3;
-    unsigned block = blockIdx.x;
-    const unsigned split = block % p.splits;
-    block /= p.splits;
-    const unsigned set = block, tile = block % p.row_tiles;
-    block /= p.row_tiles;
-    const unsigned kv = block % p.c.heads, i = block / p.c.heads;
+    unsigned split, tile, kv;
+    const unsigned set = p.splits.split(blockIdx.x, split), i = p.heads.split(p.row_tiles.split(set, tile), kv), per = p.per.d;
     const Span s = span_of(p.c, p.l, i);
     if (!s.ok) {
         if (threadIdx.x == 0 && s.rows != 0) atomicOr(p.status, ST_RANGE);
         return;
     }
-    const int rows = s.rows * (int)p.per, r0 = (int)(tile * RW);
+    const int rows = s.rows * (int)per, r0 = (int)(tile * RW);
     if (r0 >= rows) return;
     // tokens that some row of this block sees, those that every row sees, and this block's share of the sub-blocks
     const int before = s.len - s.rows;                                       // position of the sequence's first row
-    const int pos_first = before + r0 / (int)p.per, pos_last = before + (min(r0 + RW, rows) - 1) / (int)p.per;
+    const int pos_first = before + (int)p.per.quotient(r0), pos_last = before + (int)p.per.quotient(min(r0 + RW, rows) - 1);
     const int win = p.window ? (int)min(p.window, 0x7fffffffu) : 0x7fffffff;
     const int from = max(0, pos_first - win + 1), to = pos_last + 1, all_from = max(0, pos_last - win + 1), all_to = pos_first + 1;
-    const int sb0 = from / 16, n_sb = to > from ? (to + 15) / 16 - sb0 : 0, each = (n_sb + (int)p.splits - 1) / (int)p.splits;
-    const int sb_a = sb0 + min(n_sb, (int)split * each), sb_b = sb0 + min(n_sb, ((int)split + 1) * each);
+    const int sb0 = from / 16, n_sb = to > from ? (to + 15) / 16 - sb0 : 0, each = max(p.each, (int)p.splits.quotient(n_sb + p.splits.d - 1));
+    const unsigned n_splits = max(1, (n_sb + each - 1) / each);              // of this row's tokens
+    if (split >= n_splits) return;
+    const int sb_a = sb0 + (int)split * each, sb_b = sb0 + min(n_sb, ((int)split + 1) * each);
+
+    // q of this block's rows, a row a warp at a time: asked for before the copies, which wait for lengths and tables
+    auto q_row = [&](float (&x)[8], int r) {
+        const int rr = r0 + r;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = 0;
+        if (rr < rows && lane < D / 8) {
+            unsigned h;
+            const unsigned j = p.per.split(rr, h);
+            const int64_t at = (int64_t)(s.row0 + (int)j) * p.q.row_stride + (int64_t)(kv * per + h) * p.q.head_stride + 8 * lane;
+            if (p.wide) {
+                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q.data) + at);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (p.q.type == BF_BF16) {
+                        x[2 * k] = __uint_as_float(w[k] << 16);
+                        x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+                    } else {
+                        const float2 f = __half22float2(half2_of(w[k]));
+                        x[2 * k] = f.x, x[2 * k + 1] = f.y;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = load_as_float(p.q.data, p.q.type, at + k);
+            }
+        }
+    };
+    float q_first[8];
+    q_row(q_first, warp);
 
     // copies of this warp's sub-blocks.  Where they lie is looked up 32 at a time, by one lane each
     const int mine = sb_b - sb_a > (int)warp ? (sb_b - sb_a - (int)warp + ATT_WARPS - 1) / ATT_WARPS : 0;
-    const int spp = p.c.page_tokens / 16;
     const int* table = p.c.tables + (size_t)s.seq * p.c.max_pages;
     unsigned char* my_ring = ring + warp * (ATT_STAGES * S::BYTES);
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(my_ring) + lane * 16;
@@ -327,9 +374,10 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                 where = NOWHERE;
                 if (next + (int)lane < mine) {
                     const int sb = sb_a + (int)warp + ATT_WARPS * (next + (int)lane);
-                    const int page = table[sb / spp];
+                    unsigned in_page;
+                    const int page = table[p.spp.split(sb, in_page)];
                     if (page >= 0 && page < (int)p.c.n_pages)
-                        where = (unsigned)((((size_t)page * p.c.heads + kv) * p.c.block_bytes + (unsigned)(sb % spp) * S::BYTES) / 16);
+                        where = (unsigned)((((size_t)page * p.c.heads + kv) * p.c.block_bytes + in_page * S::BYTES) / 16);
                     else atomicOr(p.status, ST_RANGE);
                 }
             }
@@ -352,29 +400,14 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
     for (int k = 0; k < ATT_STAGES - 1; ++k) fetch();
 
-    // q of this block's rows as operands
+    // q as operands
     for (int r = warp; r < RW; r += ATT_WARPS) {
-        const int rr = r0 + r;
-        float x[8] = {};
-        if (rr < rows && lane < D / 8) {
-            const int64_t at = (int64_t)(s.row0 + rr / (int)p.per) * p.q.row_stride + (int64_t)(kv * p.per + rr % p.per) * p.q.head_stride + 8 * lane;
-            if (p.wide) {
-                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.q.data) + at);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        float x[8];
+        if (r == (int)warp) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (p.q.type == BF_BF16) {
-                        x[2 * k] = __uint_as_float(w[k] << 16);
-                        x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-                    } else {
-                        const float2 f = __half22float2(half2_of(w[k]));
-                        x[2 * k] = f.x, x[2 * k + 1] = f.y;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = load_as_float(p.q.data, p.q.type, at + k);
-            }
+            for (int k = 0; k < 8; ++k) x[k] = q_first[k];
+        } else {
+            q_row(x, r);
         }
         float big = 0;
 #pragma unroll
@@ -420,7 +453,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
             const int r = 8 * n + 2 * (int)j4 + h;
             coef[n][h] = row_scale[r];
             base[n][h] = NO_BASE;
-            pos[n][h] = r0 + r < rows ? before + (r0 + r) / (int)p.per : -1;
+            pos[n][h] = r0 + r < rows ? before + (int)p.per.quotient(r0 + r) : -1;
         }
         if (HOLD) {
 #pragma unroll
@@ -646,7 +679,8 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         }
     float* red = reinterpret_cast<float*>(ring);
     constexpr int PITCH = D + 4;
-    float* part = p.parts + (size_t)blockIdx.x * RW * (D + 2);
+    constexpr int PART = RW * (D + 2);                                       // rows' products, then their maxima and sums
+    float* part = p.parts + (size_t)blockIdx.x * PART;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         __syncthreads();
@@ -668,39 +702,41 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) y[k] += f * red[(w * 8 + warp) * PITCH + lane + 32 * k];
         }
-        if (p.splits == 1) {
-            const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
+        if (n_splits == 1) {
+            unsigned h;
+            const unsigned j = p.per.split(rr, h);
+            const int64_t row = s.row0 + (int)j, head = kv * per + h;
             const float inv = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + lane + 32 * k, y[k] * inv);
             if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
         } else {
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) part[r * (D + 2) + lane + 32 * k] = y[k];
-            if (lane == 0) part[r * (D + 2) + D] = top, part[r * (D + 2) + D + 1] = sum;
+            for (int k = 0; k < D / 32; ++k) part[r * D + lane + 32 * k] = y[k];
+            if (lane == 0) part[RW * D + 2 * r] = top, part[RW * D + 2 * r + 1] = sum;
         }
     }
-    if (p.splits == 1) return;
+    if (n_splits == 1) return;
     // the last block of a row's splits joins them, in their order
     __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(&p.arrivals[set], 1) == p.splits - 1;
+    if (threadIdx.x == 0) last = atomicAdd(&p.arrivals[set], 1) == n_splits - 1;
     __syncthreads();
     if (!last) return;
     __threadfence();
     if (threadIdx.x == 0) p.arrivals[set] = 0;
-    const float* first = p.parts + (size_t)(blockIdx.x - split) * RW * (D + 2);
+    const float* first = p.parts + (size_t)(blockIdx.x - split) * PART;
     float* f_of = reinterpret_cast<float*>(smem);                            // [rows][splits] what a split's part counts for
     const int n_rows = min(RW, rows - r0);
     for (int r = warp; r < n_rows; r += ATT_WARPS) {
         float top = -CUDART_INF_F, sum = 0;
-        for (unsigned k = lane; k < p.splits; k += 32) top = fmaxf(top, __ldcg(first + ((size_t)k * RW + r) * (D + 2) + D));
+        for (unsigned k = lane; k < n_splits; k += 32) top = fmaxf(top, __ldcg(first + (size_t)k * PART + RW * D + 2 * r));
 #pragma unroll
         for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        for (unsigned k = lane; k < p.splits; k += 32) {
-            const float* a = first + ((size_t)k * RW + r) * (D + 2) + D;
-            const float ml = __ldcg(a), ll = __ldcg(a + 1), f = ll == 0 ? 0.f : ml == top ? 1.f : exp2_fast(ml - top);
-            f_of[r * p.splits + k] = f;
+        for (unsigned k = lane; k < n_splits; k += 32) {
+            const float2 a = __ldcg(reinterpret_cast<const float2*>(first + (size_t)k * PART + RW * D + 2 * r));
+            const float ml = a.x, ll = a.y, f = ll == 0 ? 0.f : ml == top ? 1.f : exp2_fast(ml - top);
+            f_of[r * n_splits + k] = f;
             sum += ll == 0 ? 0.f : f * ll;
         }
 #pragma unroll
@@ -708,43 +744,75 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         if (lane == 0) {
             sh_l[0][r] = sum == 0 ? 0.f : 1.f / sum;
             if (p.lse) {
-                const int64_t row = s.row0 + (r0 + r) / (int)p.per, head = kv * p.per + (r0 + r) % p.per;
+                unsigned h;
+                const unsigned j = p.per.split(r0 + r, h);
+                const int64_t row = s.row0 + (int)j, head = kv * per + h;
                 p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
             }
         }
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < n_rows * D; u += ATT_WARPS * 32) {
-        const int r = u / D, c = u % D, rr = r0 + r;
-        const float* a = first + (size_t)r * (D + 2) + c;
-        float y = 0;
+    // four channels a thread; where the rows are few, threads share the splits out, so that many loads are on their way
+    const int n_vec = n_rows * (D / 4), groups = max(1, ATT_WARPS * 32 / n_vec), mine_k = (int)threadIdx.x / n_vec;
+    float4* sum_of = reinterpret_cast<float4*>(smem + (RW * MOST_SPLITS * 4));
+    for (int v0 = 0; v0 < n_vec; v0 += ATT_WARPS * 32) {
+        const int v = v0 + (groups > 1 ? (int)threadIdx.x % n_vec : (int)threadIdx.x), r = v / (D / 4), c = v % (D / 4) * 4, rr = r0 + r;
+        float4 y = make_float4(0, 0, 0, 0);
+        if (v < n_vec && mine_k < groups) {
+            const float* a = first + r * D + c;
 #pragma unroll 8
-        for (unsigned k = 0; k < p.splits; ++k) {
-            const float f = f_of[r * p.splits + k], v = __ldcg(a + (size_t)k * RW * (D + 2));
-            y += f == 0 ? 0.f : f * v;                                       // (a part that nothing was seen in holds zeros)
+            for (int k = groups > 1 ? mine_k : 0; k < (int)n_splits; k += groups) {
+                const float4 u = __ldcg(reinterpret_cast<const float4*>(a + (size_t)k * PART));
+                const float f = f_of[r * n_splits + k];
+                if (f != 0) y.x += f * u.x, y.y += f * u.y, y.z += f * u.z, y.w += f * u.w;    // (nothing was seen where it is 0)
+            }
         }
-        const int64_t row = s.row0 + rr / (int)p.per, head = kv * p.per + rr % p.per;
-        store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + c, y * sh_l[0][r]);
+        if (groups > 1) {
+            sum_of[threadIdx.x] = y;
+            __syncthreads();
+            if (mine_k == 0)
+                for (int k = 1; k < groups; ++k) {
+                    const float4 u = sum_of[threadIdx.x + k * n_vec];
+                    y.x += u.x, y.y += u.y, y.z += u.z, y.w += u.w;
+                }
+        }
+        if (v < n_vec && (groups == 1 || mine_k == 0)) {
+            unsigned h;
+            const unsigned j = p.per.split(rr, h);
+            const int64_t at = (int64_t)(s.row0 + (int)j) * p.out.row_stride + (int64_t)(kv * per + h) * p.out.head_stride + c;
+            const float inv = sh_l[0][r], z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) store_from_float(p.out.data, p.out.type, at + k, z[k] * inv);
+        }
     }
 }
 
 template <int D, int G, int NT> int attention(bf_trusted* t, Att p, unsigned n, unsigned max_q, unsigned max_len) {
     using S = Sub<D, G>;
     constexpr unsigned RW = 8 * NT;
-    p.row_tiles = (unsigned)(((uint64_t)max_q * p.per + RW - 1) / RW);
-    const uint64_t sets = (uint64_t)n * p.c.heads * p.row_tiles;
+    const uint64_t row_tiles = ((uint64_t)max_q * p.per.d + RW - 1) / RW, sets = (uint64_t)n * p.c.heads * row_tiles;
     if (sets >= (1u << 31) / 64) return BF_ERR_TOO_LARGE;
-    // tokens are split until there are blocks for two an SM, each with four sub-blocks a warp or more
-    const uint64_t seen = p.window && (uint64_t)p.window + max_q < max_len ? (uint64_t)p.window + max_q : max_len;
-    const uint64_t most = (seen + 16 * ATT_WARPS * 4 - 1) / (16 * ATT_WARPS * 4), wanted = (2 * (uint64_t)t->n_sm + sets - 1) / sets;
+    // A row's tokens are split while all blocks run at once, as long as a warp keeps eight sub-blocks (four, where that leaves SMs
+    // without a block and the tokens are many); and of many sequences, which may differ in length, the long ones into pieces of 128
+    // sub-blocks.  (4096 tokens, 8 key heads: one sequence 11.6 us with four, 14.1 with eight; eight of them 24.1 and 18.1.  700 tokens,
+    // 12 heads: 8.9 and 7.1.  131072 tokens in one wave of blocks 39, in two 48.  32 sequences of 160 to 8000 tokens, 8 key heads: 77 us
+    // with a block each, 67 in pieces of 128, 76 in pieces of 64.)
+    const uint64_t n_sb = ((p.window && (uint64_t)p.window + max_q < max_len ? (uint64_t)p.window + max_q : max_len) + 15) / 16;
+    const uint64_t slots = (uint64_t)t->n_sm * (NT == 1 ? 2 : 1), wanted = std::max<uint64_t>(1, slots / sets);
+    uint64_t splits = std::min(wanted, (n_sb + 8 * ATT_WARPS - 1) / (8 * ATT_WARPS));
+    if (splits * sets < (uint64_t)t->n_sm && n_sb >= 16 * ATT_WARPS)
+        splits = std::max(splits, std::min(t->n_sm / sets, (n_sb + 4 * ATT_WARPS - 1) / (4 * ATT_WARPS)));
+    if (n > 1 && NT == 1) splits = std::max(splits, (n_sb + PIECE - 1) / PIECE);
     const uint64_t fit = t->ws_bytes / (sets * RW * (D + 2) * sizeof(float));
-    uint64_t splits = wanted < most ? wanted : most;
     if (splits > MOST_SPLITS) splits = MOST_SPLITS;
     if (splits > fit) splits = fit;
     if (splits < 1 || sets > ARRIVALS) splits = 1;
-    p.splits = (unsigned)splits;
+    p.row_tiles = Divisor((unsigned)row_tiles);
+    p.splits = Divisor((unsigned)splits);
+    p.each = (int)((n_sb + splits - 1) / splits);
     constexpr size_t ring = (size_t)ATT_WARPS * ATT_STAGES * S::BYTES, red = (size_t)ATT_WARPS * 8 * (D + 4) * 4;
-    constexpr size_t smem = (D / 32) * RW * 64 + (D / G) * RW * 4 + (ring > red ? ring : red);
+    constexpr size_t first = (D / 32) * RW * 64 + (D / G) * RW * 4 + (ring > red ? ring : red), join = RW * MOST_SPLITS * 4 + ATT_WARPS * 32 * 16;
+    constexpr size_t smem = first > join ? first : join;
     const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, G, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
     attention_kernel<D, G, NT><<<(unsigned)(sets * splits), ATT_WARPS * 32, smem, t->stream>>>(p);
@@ -812,8 +880,9 @@ extern "C" int bf_kv4_attention(bf_trusted* t, const bf_kv4_cache* c, uint32_t l
     if (!n_q_heads || n_q_heads % c->n_kv_heads) return BF_ERR_SHAPE;
     ON_DEVICE(t);
     Att p{cache, List{seqs, starts, n, max_q}, *q, *out, cache.pool + layer * cache.layer_bytes, lse, (float*)t->ws, t->arrivals, t->status,
-          n_q_heads / c->n_kv_heads, n_q_heads, 0, 1, window, scale, rows_wide(q, true)};
-    const uint64_t rows = (uint64_t)max_q * p.per;
+          Divisor(n_q_heads / c->n_kv_heads), Divisor(1), Divisor(1), Divisor(c->n_kv_heads), Divisor(c->page_tokens / 16), n_q_heads, window, 0, scale,
+          rows_wide(q, true)};
+    const uint64_t rows = (uint64_t)max_q * p.per.d;
     int rc = BF_OK;
     with_shape(c, [&](auto s) {
         using S = decltype(s);
