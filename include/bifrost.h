@@ -360,6 +360,15 @@ typedef struct {
  * y another.  A non-finite x makes its row of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, CUDA. */
 int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y);
 
+/* The encrypted product from the same matrix, on the accelerator (weights are public to it): bf_encode_weights_split and bf_linear with
+ * raw weights, reading 4 bits and a scale where those read fp32 (the memory wall of Sec. 6.1: what overflows the encoded cache stays
+ * resident at an eighth of its fp32 size).  Residues are those of the fp32 matrix fma(scale, code - 8, offset), rounded once.
+ * The matrix is expanded into scratch of the context, which grows the first time a larger one is seen.
+ * bf_encode_weights_q4: bsgs_b = bsgs_g = 0 for the plan's split.  Synchronises.  bf_linear_q4: asynchronous as bf_linear is.
+ * Errors: those of the calls they stand for, and bf_q4_linear's on the matrix. */
+int bf_encode_weights_q4(bf_ctx* ctx, const bf_q4_matrix* W, uint32_t bsgs_b, uint32_t bsgs_g, bf_weights** out);
+int bf_linear_q4(bf_ctx* ctx, const uint64_t* ct_in, uint32_t n_in, const bf_q4_matrix* W, uint64_t* ct_out, uint32_t n_out);
+
 /* Keys and values of n_seqs sequences in pages of page_tokens tokens (16 to 256, a multiple of 16), one page holding a run of
  * tokens of ONE sequence, for all layers.  An element is low + scale * code, both fp16, per token, head and `group` channels.
  *   pool     device, 16-byte aligned, [n_layers][n_pages][n_kv_heads][bf_kv4_block_bytes]

@@ -153,6 +153,8 @@ _SIGNATURES = {
     "bf_trusted_status": (ctypes.c_int, [_vp]),
     "bf_trusted_last_cuda_error": (ctypes.c_char_p, [_vp]),
     "bf_q4_linear": (ctypes.c_int, [_vp, _vp, _vp, _u32, _vp]),
+    "bf_encode_weights_q4": (ctypes.c_int, [_vp, _vp, _u32, _u32, ctypes.POINTER(_vp)]),
+    "bf_linear_q4": (ctypes.c_int, [_vp, _vp, _u32, _vp, _vp, _u32]),
     "bf_kv4_block_bytes": (_u64, [_u32, _u32, _u32]),
     "bf_kv4_grow": (ctypes.c_int, [_vp, _vp, _vp, _vp, _u32]),
     "bf_kv4_append": (ctypes.c_int, [_vp, _vp, _u32, _vp, _vp, _u32, _u32, _vp, _vp]),
@@ -431,6 +433,16 @@ def bf_trusted_status(t):
 
 def bf_q4_linear(t, W: bf_q4_matrix, x: bf_rows, n: int, y: bf_rows):
     _check_trusted(load().bf_q4_linear(t, _ref(W), _ref(x), n, _ref(y)), "bf_q4_linear", t)
+
+
+def bf_encode_weights_q4(ctx, W: bf_q4_matrix, bsgs_b: int = 0, bsgs_g: int = 0):
+    out = _vp()
+    _check(load().bf_encode_weights_q4(ctx, _ref(W), bsgs_b, bsgs_g, ctypes.byref(out)), "bf_encode_weights_q4", ctx)
+    return out
+
+
+def bf_linear_q4(ctx, ct_in, n_in: int, W: bf_q4_matrix, ct_out, n_out: int):
+    _check(load().bf_linear_q4(ctx, _ptr(ct_in), n_in, _ref(W), _ptr(ct_out), n_out), "bf_linear_q4", ctx)
 
 
 def bf_kv4_block_bytes(head_dim: int, group: int, page_tokens: int) -> int:

@@ -11,6 +11,7 @@
 
 #include "../../include/bifrost.h"
 #include "bf_host.h"
+#include "bf_trusted.h"
 
 using namespace bf;
 
@@ -118,7 +119,7 @@ struct bf_ctx {
     std::vector<u32> gal, gal_inv;   // Galois element of each key's rotation, 5^steps mod 2N, and its inverse
     u32 n_keys = 0;
     // scratch (grow-only)
-    DevBuf X, X0, Aext, Dig, U, Ubig, Tc, Tn, Cc, A, Lfull, fft, coef, ptnat, ptjit, stage_in, stage_out, nm_a, nm_b;
+    DevBuf X, X0, Aext, Dig, U, Ubig, Tc, Tn, Cc, A, Lfull, fft, coef, ptnat, ptjit, stage_in, stage_out, nm_a, nm_b, w32;
     u64 cache_budget = 0, cache_used = 0;
     std::vector<bf_weights*> weights;
     std::string cuda_msg;
@@ -450,7 +451,7 @@ extern "C" void bf_ctx_destroy(bf_ctx* ctx) {
         }
     }
     DevBuf* bufs[] = {&ctx->X, &ctx->X0, &ctx->Aext, &ctx->Dig, &ctx->U, &ctx->Ubig, &ctx->Tc, &ctx->Tn, &ctx->Cc, &ctx->A, &ctx->Lfull,
-                      &ctx->fft, &ctx->coef, &ctx->ptnat, &ctx->ptjit, &ctx->stage_in, &ctx->stage_out, &ctx->nm_a, &ctx->nm_b};
+                      &ctx->fft, &ctx->coef, &ctx->ptnat, &ctx->ptjit, &ctx->stage_in, &ctx->stage_out, &ctx->nm_a, &ctx->nm_b, &ctx->w32};
     for (DevBuf* b : bufs) free_buf(*b);
     cudaFree(ctx->tw_fwd);
     cudaFree(ctx->tw_inv);
@@ -775,6 +776,34 @@ extern "C" int bf_encode_weights_split(bf_ctx* ctx, const float* W, uint32_t d_o
     ctx->weights.push_back(w);
     *out = w;
     return BF_OK;
+}
+
+// the fp32 matrix that a 4-bit one stands for, in scratch
+static int expand_q4(bf_ctx* ctx, const bf_q4_matrix* W) {
+    TRY(bft::q4_check(W));
+    TRY(ensure(ctx, ctx->w32, (size_t)W->d_out * W->d_in * sizeof(float)));
+    CK(bft::launch_q4_expand(*W, (float*)ctx->w32.p, ctx->stream));
+    return BF_OK;
+}
+
+extern "C" int bf_encode_weights_q4(bf_ctx* ctx, const bf_q4_matrix* W, uint32_t bsgs_b, uint32_t bsgs_g, bf_weights** out) {
+    if (!ctx || !out) return BF_ERR_INVALID_ARG;
+    *out = nullptr;
+    TRY(bft::q4_check(W));
+    if (!bsgs_b && !bsgs_g) bsgs_b = ctx->plan.bsgs_b, bsgs_g = ctx->plan.bsgs_g;
+    if (!split_ok(ctx, bsgs_b, bsgs_g)) return BF_ERR_SHAPE;
+    // (nothing is expanded for a matrix that the budget has no room for)
+    if (ctx->cache_budget && ctx->cache_used + weights_bytes(ctx, W->d_out, W->d_in, bsgs_b, bsgs_g) > ctx->cache_budget) return BF_ERR_OOM;
+    TRY(expand_q4(ctx, W));
+    return bf_encode_weights_split(ctx, (const float*)ctx->w32.p, W->d_out, W->d_in, bsgs_b, bsgs_g, out);
+}
+
+extern "C" int bf_linear_q4(bf_ctx* ctx, const uint64_t* ct_in, uint32_t n_in, const bf_q4_matrix* W, uint64_t* ct_out, uint32_t n_out) {
+    if (!ctx || !ct_in || !ct_out) return BF_ERR_INVALID_ARG;
+    TRY(bft::q4_check(W));
+    if (n_in != cdiv(W->d_in, ctx->plan.tile_D) || n_out != n_out_cts(ctx, W->d_out)) return BF_ERR_SHAPE;
+    TRY(expand_q4(ctx, W));
+    return bf_linear(ctx, ct_in, n_in, nullptr, (const float*)ctx->w32.p, W->d_out, W->d_in, ct_out, n_out);
 }
 
 extern "C" void bf_weights_free(bf_ctx* ctx, bf_weights* w) {

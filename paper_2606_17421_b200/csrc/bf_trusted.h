@@ -57,6 +57,10 @@ inline bool rows_wide(const bf_rows* r, bool heads) {
     return (uintptr_t)r->data % 16 == 0 && r->row_stride % per == 0 && (!heads || r->head_stride % per == 0);
 }
 
+// ---- q4.cu
+int q4_check(const bf_q4_matrix* W);
+cudaError_t launch_q4_expand(const bf_q4_matrix& W, float* out, cudaStream_t stream);      // out: [d_out][d_in]
+
 // The cache as kernels take it.
 struct Cache {
     unsigned char* pool;

@@ -646,17 +646,43 @@ template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_r
 
 }  // namespace
 
-extern "C" int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y) {
-    if (!t || !W || !n || !rows_ok(x) || !rows_ok(y) || !W->codes || !W->scales || !W->d_out || !W->d_in) return BF_ERR_INVALID_ARG;
+// One thread an element; read from L2 and L1, bound by the writes.
+static __global__ void __launch_bounds__(256) q4_expand_kernel(Q4 w, float* out) {
+    const unsigned c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= w.d_in) return;
+    for (unsigned o = blockIdx.y; o < w.d_out; o += gridDim.y) {
+        const int code = w.codes[o * w.row_bytes + c / 2] >> (4 * (c % 2)) & 15;
+        const size_t g = (size_t)o * w.group_stride + c / w.group;
+        out[(size_t)o * w.d_in + c] = fmaf(__half2float(w.scales[g]), (float)(code - 8), w.offsets ? __half2float(w.offsets[g]) : 0.f);
+    }
+}
+
+static Q4 q4_of(const bf_q4_matrix& W) {
+    return Q4{W.codes, (const __half*)W.scales, (const __half*)W.offsets, W.row_bytes, W.group_stride, W.d_out, W.d_in, W.group};
+}
+
+cudaError_t bft::launch_q4_expand(const bf_q4_matrix& W, float* out, cudaStream_t stream) {
+    q4_expand_kernel<<<dim3((W.d_in + 255) / 256, W.d_out < 65535 ? W.d_out : 65535), 256, 0, stream>>>(q4_of(W), out);
+    return cudaGetLastError();
+}
+
+int bft::q4_check(const bf_q4_matrix* W) {
+    if (!W || !W->codes || !W->scales || !W->d_out || !W->d_in) return BF_ERR_INVALID_ARG;
     if ((uintptr_t)W->codes % 16 || (uintptr_t)W->scales % 16 || (uintptr_t)W->offsets % 16) return BF_ERR_INVALID_ARG;
     if (W->group != 32 && W->group != 64 && W->group != 128) return BF_ERR_SHAPE;
     const uint32_t groups = W->d_in / W->group + (W->d_in % W->group != 0);
     if (W->row_bytes % 16 || W->row_bytes < W->d_in / 2 + W->d_in % 2 || W->group_stride % 8 || W->group_stride < groups) return BF_ERR_SHAPE;
     // rows are counted in 31 bits, and the tail of a stage of columns behind d_in stays in them too
-    if (n >= (1u << 31) || W->d_out >= (1u << 31) - 4096 || W->d_in >= (1u << 31) - 4096 || W->row_bytes >= (1ull << 32)) return BF_ERR_SHAPE;
+    return W->d_out >= (1u << 31) - 4096 || W->d_in >= (1u << 31) - 4096 || W->row_bytes >= (1ull << 32) ? BF_ERR_SHAPE : BF_OK;
+}
+
+extern "C" int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y) {
+    if (!t || !n || !rows_ok(x) || !rows_ok(y)) return BF_ERR_INVALID_ARG;
+    if (int rc = q4_check(W)) return rc;
+    if (n >= (1u << 31)) return BF_ERR_SHAPE;
     OnDevice on(t->device);
     if (!on.ok) return cuda_failed(t, "cudaSetDevice", cudaErrorInvalidDevice);
-    const Q4 w{W->codes, (const __half*)W->scales, (const __half*)W->offsets, W->row_bytes, W->group_stride, W->d_out, W->d_in, W->group};
+    const Q4 w = q4_of(*W);
     switch (W->group) {
         case 32: return W->offsets ? linear<32, true>(t, w, *x, n, *y) : linear<32, false>(t, w, *x, n, *y);
         case 64: return W->offsets ? linear<64, true>(t, w, *x, n, *y) : linear<64, false>(t, w, *x, n, *y);

@@ -22,6 +22,81 @@ def _uniform_residues(gen: torch.Generator, moduli, lead_shape, N: int, device) 
     return out
 
 
+class TrustedHalf:
+    """The trusted domain's part of a decode step, on a GPU of its own in earnest: in every layer the new token's keys and values
+    appended to a cache in 4 bits and attention over it, behind the last layer the vocabulary projection from 4-bit weights.
+    What it would get by decryption (rows of q, k and v; the last hidden state) is drawn once and stands in for it."""
+
+    def __init__(self, name: str, seqs: int = 1, context: int = 512, room: int = 512, group: int = 64, page_tokens: int = 64, seed: int = 0,
+                 device: str = "cuda:0", stream: torch.cuda.Stream | None = None):
+        m = self.model = wl.DECODERS[name]
+        self.layers, self.seqs, self.context, self.most = wl.WORKLOADS[name].n_repeat, seqs, context, context + room
+        self.device = torch.device(device)
+        torch.cuda.set_device(self.device)
+        self.stream = stream or torch.cuda.Stream(device=self.device)
+        with torch.cuda.stream(self.stream):
+            gen = torch.Generator(device=self.device)
+            gen.manual_seed(seed)
+            self.ctx = bf.bf_trusted_create(0, self.stream.cuda_stream)
+            max_pages = wl.ceil_div(self.most, page_tokens)
+            n_pages = seqs * max_pages
+            self.pool = torch.zeros((self.layers, n_pages, m.kv_heads, bf.bf_kv4_block_bytes(m.head_dim, group, page_tokens)),
+                                    dtype=torch.uint8, device=self.device)
+            self.tables = torch.full((seqs, max_pages), -1, dtype=torch.int32, device=self.device)
+            self.lengths = torch.zeros(seqs, dtype=torch.int32, device=self.device)
+            self.refs = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
+            self.cache = bf.bf_kv4_cache.of(self.pool, self.tables, self.lengths, self.refs, m.head_dim, group, page_tokens)
+            self.all_seqs = torch.arange(seqs, dtype=torch.int32, device=self.device)
+            rows = torch.randn((seqs, m.heads + 2 * m.kv_heads, m.head_dim), generator=gen, device=self.device).bfloat16()
+            self.qkv, (self.q, self.k, self.v) = rows, rows.split([m.heads, m.kv_heads, m.kv_heads], 1)
+            self.attended = torch.empty((seqs, m.heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
+            self.hidden = torch.randn((seqs, m.hidden), generator=gen, device=self.device).bfloat16()
+            self.logits = torch.empty((seqs, m.vocab), dtype=torch.float32, device=self.device)
+            codes, scales = wl.gen_q4_weights(seed, "vocab", m.vocab, m.hidden, group)
+            self.codes, self.scales = torch.from_numpy(codes).to(self.device), torch.from_numpy(scales).to(self.device)
+            self.head = bf.bf_q4_matrix.of(self.codes, self.scales, None, m.hidden, group)
+            self.length = 0
+            self._prompt(gen)
+
+    def _prompt(self, gen):
+        """Fills the cache with `context` tokens of every sequence."""
+        self._grow(self.context)
+        m, n = self.model, self.seqs * self.context
+        starts = torch.arange(self.seqs + 1, dtype=torch.int32, device=self.device) * self.context
+        for layer in range(self.layers):
+            k, v = torch.randn((2, n, m.kv_heads, m.head_dim), generator=gen, device=self.device).bfloat16()
+            bf.bf_kv4_append(self.ctx, self.cache, layer, None, starts, self.seqs, self.context, bf.bf_rows.of(k), bf.bf_rows.of(v))
+        bf.bf_trusted_status(self.ctx)
+
+    def _grow(self, tokens: int):
+        counts = None if tokens == 1 else torch.full((self.seqs,), tokens, dtype=torch.int32, device=self.device)
+        bf.bf_kv4_grow(self.ctx, self.cache, None, counts, self.seqs)
+        self.length += tokens
+
+    def begin(self):
+        """Room for the step's token.  A cache that is full starts over from the prompt's length (and keeps its bytes)."""
+        if self.length == self.most:
+            bf.bf_kv4_free(self.ctx, self.cache, self.all_seqs, self.seqs)
+            self.length = 0
+            self._grow(self.context)
+        self._grow(1)
+
+    def attend(self, layer: int):
+        """Between the q/k/v product of a layer and its output product."""
+        m = self.model
+        bf.bf_kv4_append(self.ctx, self.cache, layer, None, None, self.seqs, 1, bf.bf_rows.of(self.k), bf.bf_rows.of(self.v))
+        bf.bf_kv4_attention(self.ctx, self.cache, layer, None, None, self.seqs, 1, self.length, bf.bf_rows.of(self.q), m.heads,
+                            bf.bf_rows.of(self.attended), m.head_dim ** -0.5)
+
+    def finish(self):
+        """Logits of the step."""
+        bf.bf_q4_linear(self.ctx, self.head, bf.bf_rows.of(self.hidden), self.seqs, bf.bf_rows.of(self.logits))
+
+    def close(self):
+        bf.bf_trusted_status(self.ctx)
+        bf.bf_trusted_destroy(self.ctx)
+
+
 class WorkloadRunner:
     """One context per workload; per layer: weights (cached when the budget allows), input and
     output ciphertext buffers."""
@@ -30,7 +105,7 @@ class WorkloadRunner:
                  cache_budget_bytes: int | None = None, stream: torch.cuda.Stream | None = None,
                  fuse_shared_inputs: bool = True, fold_in_ciphertext: bool = False, compact_cache: bool = False,
                  pack: str | None = None, moddown: str | None = None, hoist: str | None = None, coef_bits: int = 0,
-                 lanes: int | None = None):
+                 lanes: int | None = None, q4_group: int = 0, trusted: TrustedHalf | None = None):
         self.w = wl.WORKLOADS[name]
         ps = wl.PARAM_SETS[self.w.params]
         self.N, self.primes, self.P, self.scale = ps["N"], list(ps["primes"]), ps["special"], ps["scale"]
@@ -93,18 +168,26 @@ class WorkloadRunner:
             del keys
         self.key_bytes = len(self.rot_steps) * self.r * 2 * self.N * sum(5 if q < 2 ** 40 else 8 for q in basis)
         # layers
+        self.trusted = trusted
         self.layers = []
         for rep in range(self.w.n_repeat):
             for L in units:
                 n_in, n_out = wl.ceil_div(L.d_in, D), wl.ceil_div(L.d_out, self.plan.rows_per_ct)
-                W = torch.from_numpy(np.concatenate(
-                    [wl.gen_weights(seed, f"{m.name}.{rep}", m.d_out, m.d_in) for m in members_of[L.name]], axis=0)
-                ).to(self.device)
+                W, q4 = None, None
+                if q4_group:            # a quantised checkpoint: what is encoded comes from 4 bits, and what is not cached stays in them
+                    parts = [wl.gen_q4_weights(seed, f"{m.name}.{rep}", m.d_out, m.d_in, q4_group) for m in members_of[L.name]]
+                    q4_data = [torch.from_numpy(np.concatenate(a, axis=0)).to(self.device) for a in zip(*parts)]
+                    q4 = (bf.bf_q4_matrix.of(*q4_data, None, L.d_in, q4_group), q4_data)
+                else:
+                    W = torch.from_numpy(np.concatenate(
+                        [wl.gen_weights(seed, f"{m.name}.{rep}", m.d_out, m.d_in) for m in members_of[L.name]], axis=0)
+                    ).to(self.device)
                 handle = None
                 b, g = self.splits[L.name]
                 if cache:
                     try:
-                        handle = bf.bf_encode_weights_split(self.ctx, W, L.d_out, L.d_in, b, g)
+                        handle = bf.bf_encode_weights_q4(self.ctx, q4[0], b, g) if q4 else \
+                            bf.bf_encode_weights_split(self.ctx, W, L.d_out, L.d_in, b, g)
                     except bf.BifrostError as e:
                         if e.code != bf.BF_ERR_OOM:
                             raise
@@ -113,7 +196,7 @@ class WorkloadRunner:
                 ct_in = _uniform_residues(self.gen, self.primes, (n_in, 2), self.N, self.device)
                 ct_out = torch.empty((n_out, 2, self.r, self.N), dtype=torch.int64, device=self.device)
                 ct_low = torch.empty((n_out, 2, self.r - 1, self.N), dtype=torch.int64, device=self.device)
-                self.layers.append(dict(layer=L, rep=rep, n_in=n_in, n_out=n_out, b=b, g=g, W=W, handle=handle,
+                self.layers.append(dict(layer=L, rep=rep, n_in=n_in, n_out=n_out, b=b, g=g, W=W, q4=q4, handle=handle,
                                         ct_in=ct_in, ct_out=ct_out, ct_low=ct_low,
                                         pt_bytes=n_in * n_out * (D // self.plan.tau) * self.N * self.word_bytes,
                                         resident_bytes=n_in * n_out * (D // self.plan.tau) * self.N *
@@ -123,17 +206,33 @@ class WorkloadRunner:
     # ------------------------------------------------------------------ one decode token
     def step(self):
         """All linear layers of the workload once: the product and its rescale per layer (device buffers), as the one
-        call that does both unless the in-ciphertext fold sits between them."""
-        for e in self.layers:
-            L = e["layer"]
-            if not self.fold_in_ciphertext:
-                bf.bf_linear_rescaled(self.ctx, e["ct_in"], e["n_in"], e["handle"], None if e["handle"] else e["W"],
-                                      L.d_out, L.d_in, e["ct_low"], e["n_out"])
-                continue
-            bf.bf_linear(self.ctx, e["ct_in"], e["n_in"], e["handle"], None if e["handle"] else e["W"],
-                         L.d_out, L.d_in, e["ct_out"], e["n_out"])
-            bf.bf_fold(self.ctx, e["ct_out"], e["n_out"])
+        call that does both unless the in-ciphertext fold sits between them or the weights come from 4 bits.  With a trusted half,
+        its attention follows the first call of each layer and its projection the last of all."""
+        if self.trusted:
+            self.trusted.begin()
+        for i, e in enumerate(self.layers):
+            self._call(e)
+            if self.trusted and (i == 0 or self.layers[i - 1]["rep"] != e["rep"]):
+                self.trusted.attend(e["rep"])
+        if self.trusted:
+            self.trusted.finish()
+
+    def _call(self, e):
+        L = e["layer"]
+        if e["q4"] and not e["handle"]:
+            bf.bf_linear_q4(self.ctx, e["ct_in"], e["n_in"], e["q4"][0], e["ct_out"], e["n_out"])
+            if self.fold_in_ciphertext:
+                bf.bf_fold(self.ctx, e["ct_out"], e["n_out"])
             bf.bf_rescale(self.ctx, e["ct_out"], e["ct_low"], e["n_out"], self.r)
+            return
+        if not self.fold_in_ciphertext:
+            bf.bf_linear_rescaled(self.ctx, e["ct_in"], e["n_in"], e["handle"], None if e["handle"] else e["W"],
+                                  L.d_out, L.d_in, e["ct_low"], e["n_out"])
+            return
+        bf.bf_linear(self.ctx, e["ct_in"], e["n_in"], e["handle"], None if e["handle"] else e["W"],
+                     L.d_out, L.d_in, e["ct_out"], e["n_out"])
+        bf.bf_fold(self.ctx, e["ct_out"], e["n_out"])
+        bf.bf_rescale(self.ctx, e["ct_out"], e["ct_low"], e["n_out"], self.r)
 
     def make_host_buffers(self):
         for e in self.layers:
@@ -141,7 +240,7 @@ class WorkloadRunner:
             e["h_out"] = torch.empty((e["n_out"], 2, self.r - 1, self.N), dtype=torch.int64).pin_memory()
 
     def step_host(self):
-        """The same through the host-buffer entry point: ciphertexts travel host -> device -> host."""
+        """The products (with fp32 or cached weights) through the host-buffer entry point: ciphertexts travel host -> device -> host."""
         for e in self.layers:
             L = e["layer"]
             bf.bf_linear_host(self.ctx, e["h_in"], e["n_in"], e["handle"], None if e["handle"] else e["W"],

@@ -89,6 +89,21 @@ LLAMA3_8B_LAYER = (Layer("q", 4096, 4096, "attn"), Layer("k", 4096, 1024, "attn"
                    Layer("down", 14336, 4096))
 
 
+@dataclass(frozen=True)
+class Decoder:
+    """What the trusted half of a decode step needs to know of a model."""
+    heads: int
+    kv_heads: int
+    head_dim: int
+    hidden: int
+    vocab: int
+
+
+GPT2 = Decoder(12, 12, 64, 768, 50257)
+QWEN3 = Decoder(16, 8, 128, 1024, 151936)
+LLAMA3_8B = Decoder(32, 8, 128, 4096, 128256)
+
+
 def fuse_shared_inputs(layers, D: int):
     """Group consecutive projections that read the same activation: [(fused name, d_in, [member layers])].
     Members must have d_out a multiple of the tile side D so that their row blocks stay aligned."""
@@ -134,6 +149,7 @@ WORKLOADS["gpt2_qkv_paper_params"] = Workload("gpt2_qkv_paper_params", "paper_n1
 # several passes, with the call shapes of the whole step (one and three input ciphertexts, one and three output blocks).
 WORKLOADS["gpt2_layer"] = Workload("gpt2_layer", "n15", PlanSpec(1024, 16, 16, 4), GPT2_LAYER,
                                    splits={"ffn_down": (8, 8)})
+DECODERS = {"gpt2_qkv": GPT2, "gpt2_step": GPT2, "gpt2_layer": GPT2, "qwen3_step": QWEN3, "llama3_layer": LLAMA3_8B}
 CONFIG_ORDER = ["tiny", "gpt2_qkv", "gpt2_step", "qwen3_step", "llama3_layer"]
 
 
@@ -149,6 +165,20 @@ def _stream(seed: int, *tag) -> np.random.Generator:
 def gen_weights(seed: int, tag, d_out: int, d_in: int) -> np.ndarray:
     """fp32 W[d_out][d_in] ~ N(0, 0.02^2)."""
     return (_stream(seed, "W", tag).standard_normal((d_out, d_in)) * 0.02).astype(np.float32)
+
+
+def gen_q4_weights(seed: int, tag, d_out: int, d_in: int, group: int):
+    """The same in 4 bits, as a quantised checkpoint has them: codes uint8 [d_out][bytes of a row], two columns a byte, and scales
+    float16 [d_out][groups, a multiple of 8], weight = scale * (code - 8)."""
+    w = gen_weights(seed, tag, d_out, d_in)
+    groups, cols = ceil_div(d_in, group), ceil_div(d_in, 32) * 32
+    w = np.pad(w, ((0, 0), (0, groups * group - d_in))).reshape(d_out, groups, group)
+    scale = (np.abs(w).max(-1) / 7).astype(np.float16)
+    code = np.clip(np.rint(w / np.maximum(scale, np.float16(1e-6))[..., None].astype(np.float32)) + 8, 0, 15).astype(np.uint8).reshape(d_out, -1)
+    code = np.pad(code, ((0, 0), (0, max(0, cols - code.shape[1]))), constant_values=8)[:, :cols]
+    scales = np.zeros((d_out, ceil_div(groups, 8) * 8), np.float16)
+    scales[:, :groups] = scale
+    return np.ascontiguousarray(code[:, 0::2] | code[:, 1::2] << 4), scales
 
 
 def gen_activation(seed: int, tag, d_in: int) -> np.ndarray:

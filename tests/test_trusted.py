@@ -780,3 +780,141 @@ def test_two_contexts_on_two_streams(side):
     for got, w in zip(outs, want):
         assert all(torch.equal(o, w) for o in got)
     bf.bf_trusted_destroy(t2)
+
+
+# ---- the encrypted product from the same 4-bit matrix, and the runner
+
+@gpu
+@pytest.mark.parametrize("offsets", [False, True])
+def test_encrypted_product_from_4_bits_is_that_of_the_matrix_it_stands_for(offsets):
+    """Residues of cached and on-the-fly products from 4 bits equal those from the fp32 matrix, bit for bit; refusals."""
+    import torch
+    from paper_2606_17421_b200 import workloads as wl
+    rng = np.random.default_rng(4)
+    d_out, d_in = 70, 100
+    packed, scales, offs, _, _ = draw_matrix(rng, d_out, d_in, 32, offsets)
+    code = np.stack([packed & 15, packed >> 4], -1).reshape(d_out, -1)[:, :d_in].astype(np.float32)
+    g = np.arange(d_in) // 32
+    # one rounding to fp32: products of an 11-bit scale and a 4-bit code are exact, so an fp64 sum rounds once too
+    W = (scales[:, g].astype(np.float64) * (code - 8) + (offs[:, g].astype(np.float64) if offsets else 0)).astype(np.float32)
+    ps = wl.PARAM_SETS["n12"]
+    N, primes, r = ps["N"], list(ps["primes"]), len(ps["primes"])
+    ctx = bf.bf_ctx_create(N, primes + [ps["special"]], r, ps["scale"], bf.bf_plan(64, 1, 8, 8), torch.cuda.current_stream().cuda_stream)
+    try:
+        steps = [k for k in range(1, 8)] + [8 * j for j in range(1, 8)]
+        gen = torch.Generator(device="cuda").manual_seed(0)
+
+        def residues(*lead, moduli):
+            return torch.stack([torch.randint(0, q, (*lead, N), generator=gen, device="cuda") for q in moduli], -2)
+
+        keys = residues(len(steps), r, 2, moduli=primes + [ps["special"]])
+        bf.bf_load_eval_keys(ctx, steps, len(steps), keys)
+        ct = residues(2, 2, moduli=primes)
+        codes, sc, of, w32 = (None if a is None else torch.from_numpy(a).cuda() for a in (packed, scales, offs, W))
+        M = bf.bf_q4_matrix.of(codes, sc, of, d_in, 32)
+        want, got = torch.empty((2, 2, r, N), dtype=torch.int64, device="cuda"), torch.zeros((2, 2, r, N), dtype=torch.int64, device="cuda")
+        bf.bf_linear(ctx, ct, 2, None, w32, d_out, d_in, want, 2)
+        bf.bf_linear_q4(ctx, ct, 2, M, got, 2)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and bool((want != 0).any())
+        for split in ((0, 0), (8, 8)):
+            h = bf.bf_encode_weights_q4(ctx, M, *split)
+            got.zero_()
+            bf.bf_linear(ctx, ct, 2, h, None, d_out, d_in, got, 2)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+            bf.bf_weights_free(ctx, h)
+        refused(bf.BF_ERR_SHAPE, bf.bf_linear_q4, ctx, ct, 1, M, got, 2)
+        refused(bf.BF_ERR_INVALID_ARG, bf.bf_linear_q4, ctx, None, 2, M, got, 2)
+        refused(bf.BF_ERR_SHAPE, bf.bf_encode_weights_q4, ctx, M, 4, 4)
+        refused(bf.BF_ERR_INVALID_ARG, bf.bf_encode_weights_q4, ctx, matrix(codes=None))
+        refused(bf.BF_ERR_SHAPE, bf.bf_encode_weights_q4, ctx, matrix(group=16))
+        bf.bf_set_cache_budget(ctx, 1000)
+        refused(bf.BF_ERR_OOM, bf.bf_encode_weights_q4, ctx, M)
+    finally:
+        bf.bf_ctx_destroy(ctx)
+
+
+@gpu
+def test_runner_with_its_trusted_half():
+    """A step of the runner: the encrypted products as without the trusted half, attention and logits as direct calls give them, and a
+    cache that starts over when it is full."""
+    import torch
+    from paper_2606_17421_b200.runner import TrustedHalf, WorkloadRunner
+    stream = torch.cuda.Stream()
+    half = TrustedHalf("gpt2_qkv", seqs=2, context=30, room=3, page_tokens=16, stream=stream)
+    R = WorkloadRunner("gpt2_qkv", stream=stream, trusted=half, q4_group=64)
+    try:
+        lens = []
+        for _ in range(5):
+            R.step()
+            torch.cuda.synchronize()
+            lens.append(half.lengths.tolist())
+        assert lens == [[31] * 2, [32] * 2, [33] * 2, [31] * 2, [32] * 2]
+        low = R.layers[0]["ct_low"].clone()
+        R.trusted = None
+        R.layers[0]["ct_low"].zero_()
+        R.step()
+        torch.cuda.synchronize()
+        assert torch.equal(low, R.layers[0]["ct_low"])
+        W = np.stack([half.codes.cpu().numpy() & 15, half.codes.cpu().numpy() >> 4], -1).reshape(half.codes.shape[0], -1)[:, :768].astype(np.float64) - 8
+        W *= half.scales.cpu().numpy().astype(np.float64)[:, np.arange(768) // 64]
+        x = half.hidden.double().cpu().numpy()
+        assert (np.abs(half.logits.double().cpu().numpy() - x @ W.T) <= linear_tolerance(x, x @ W.T, 3 * np.abs(W) + W.std(), "fp32")).all()
+        assert torch.isfinite(half.attended.float()).all() and int(half.refs.sum()) == 4
+    finally:
+        R.close()
+        half.close()
+
+
+@gpu
+def test_runner_from_4_bits_beyond_the_cache_budget():
+    """What the encoded cache has no room for is encoded from 4 bits inside the call: the same ciphertexts."""
+    import torch
+    from paper_2606_17421_b200.runner import WorkloadRunner
+    out = []
+    for budget in (None, 1):
+        R = WorkloadRunner("gpt2_qkv", q4_group=32, cache_budget_bytes=budget)
+        try:
+            assert R.n_fallback_layers() == (0 if budget is None else 1)
+            R.step()
+            torch.cuda.synchronize()
+            out.append(R.layers[0]["ct_low"].clone())
+        finally:
+            R.close()
+    assert torch.equal(*out)
+
+
+@gpu
+def test_attention_keeps_a_nan_to_the_rows_that_see_it(side):
+    """Tokens with a NaN in a group of their values or keys: rows that do not see them, and other groups, stay as they are."""
+    torch = side.torch
+    for D, G, heads in ((64, 32, 2), (128, 128, 12)):
+        c = ref.Cache(1, 12, 1, D, G, 16, 1, 10)
+        d = fill(side, c, [120], seed=1)
+        q = torch.randn((9, heads, D), device="cuda").half()
+        st = side.ints([0, 9])
+
+        def run(cache, window):
+            out = torch.zeros((9, heads, D), device="cuda").half()
+            bf.bf_kv4_attention(side.t, cache.desc, 0, None, st, 1, 9, 120, bf.bf_rows.of(q), heads, bf.bf_rows.of(out), D ** -0.5, window, None)
+            return side.host(out)
+
+        for window in (0, 5):
+            clean = run(d, window)
+            block = c.tables[0, 115 // 16]
+            sub = c.pool[0, block, 0, 0]
+            keep = sub.copy()
+            sub.view(np.float16)[c.vp[115 % 16, (D // G) - 1]] = np.nan                   # the last group of token 115's values
+            bad = run(DeviceCache(side, c), window)
+            sub[:] = keep
+            sees = np.array([115 <= 111 + j and (not window or 115 > 111 + j - window) for j in range(9)])
+            assert np.isnan(bad[sees][:, :, D - G:]).all()
+            assert np.array_equal(bad[~sees], clean[~sees])
+            if G < D:
+                assert np.isfinite(bad[sees][:, :, :D - G]).all()
+            sub.view(np.float16)[c.kp[115 % 16, 0]] = np.nan                              # its keys
+            bad = run(DeviceCache(side, c), window)
+            sub[:] = keep
+            assert np.isnan(bad[sees]).all() and np.array_equal(bad[~sees], clean[~sees])
+    assert status_of(side) == 0
