@@ -40,15 +40,69 @@ template <int D, int G> struct Sub {
     static constexpr int K_PAR = 8 * D, V_CODE = 8 * D + 64 * E, V_PAR = 16 * D + 64 * E, BYTES = 16 * D + 128 * E;
 };
 
-constexpr unsigned IO_THREADS = 128;
+// ------------------------------------------------------------------------------------------------
+// Writing and reading.  One block a (sub-block, head); D / 8 lanes a token, 8 channels a lane, 16 or 32 bytes to a load or store.  Both are
+// bound by what they move; what a sub-block holds is put together in, or taken from, shared memory, so that the cache sees whole lines.
+constexpr int IO_THREADS = 128;
 
-// One block a (sub-block, head): a warp takes a (token, group) at a time, finds its range, leaves the codes in shared memory;
-// then whole words of codes are put together, since a word of value codes holds four tokens of two channels.
+__device__ __forceinline__ void load8(float (&x)[8], const bf_rows& r, int64_t at, bool wide) {
+    if (wide && r.type == BF_F32) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(r.data) + at);
+        const float4 a = p[0], b = p[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else if (wide) {
+        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(r.data) + at);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (r.type == BF_BF16) {
+                x[2 * k] = __uint_as_float(w[k] << 16);
+                x[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                x[2 * k] = f.x, x[2 * k + 1] = f.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = load_as_float(r.data, r.type, at + k);
+    }
+}
+__device__ __forceinline__ void store8(const float (&x)[8], const bf_rows& r, int64_t at, bool wide) {
+    if (wide && r.type == BF_F32) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(r.data) + at);
+        p[0] = make_float4(x[0], x[1], x[2], x[3]);
+        p[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else if (wide) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (r.type == BF_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+                w[k] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __half2 h = __floats2half2_rn(x[2 * k], x[2 * k + 1]);
+                w[k] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(r.data) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) store_from_float(r.data, r.type, at + k, x[k]);
+    }
+}
+// eight bytes below 16, the first in the lowest bits -> eight nibbles
+__device__ __forceinline__ uint32_t nibbles_of(uint2 v) {
+    const uint32_t a = (v.x | v.x >> 4) & 0x00ff00ffu, b = (v.y | v.y >> 4) & 0x00ff00ffu;
+    return __byte_perm(a, b, 0x6420);
+}
+
 template <int D, int G>
-__global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned layer, List l, unsigned subs, bf_rows k, bf_rows v, int* status) {
+__global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned layer, List l, unsigned subs, bf_rows k, bf_rows v, int wide, int* status) {
     using S = Sub<D, G>;
-    __shared__ unsigned char code[2][16][D];
-    const unsigned i = blockIdx.x / subs, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int LANES = D / 8, UNITS = IO_THREADS / LANES;                 // lanes of a token; tokens at once
+    __shared__ __align__(16) unsigned char image[S::BYTES], code[16 * D];    // code: a byte a nibble of the value words
+    const unsigned i = blockIdx.x / subs, head = blockIdx.y;
     const Span s = span_of(c, l, i);
     bool twice = false;
     if (l.seqs)
@@ -67,97 +121,93 @@ __global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned la
         return;
     }
     unsigned char* out = c.pool + layer * c.layer_bytes + ((size_t)page * c.heads + head) * c.block_bytes + (t0 % c.page_tokens) / 16 * S::BYTES;
-    for (int u = warp; u < 2 * (to - from) * S::E; u += IO_THREADS / 32) {
-        const int e = u % S::E, kind = u / S::E % 2, tok = from + u / (2 * S::E);
-        const bf_rows& r = kind ? v : k;
-        const int64_t at = (int64_t)(s.row0 + t0 + tok - base) * r.row_stride + head * r.head_stride + e * G + lane;
-        float x[G / 32], low = CUDART_INF_F, high = -CUDART_INF_F;
+    const int ch = (int)threadIdx.x % LANES * 8, unit = (int)threadIdx.x / LANES;
+#pragma unroll 4
+    for (int u0 = 2 * from; u0 < 2 * to; u0 += UNITS) {                      // key of token u / 2, value of it
+        const int u = u0 + unit, kind = u & 1, tok = u >> 1, e = ch / G;
+        const bool here = tok < to;
+        float x[8] = {}, low = CUDART_INF_F, high = -CUDART_INF_F;
+        if (here) load8(x, kind ? v : k, (int64_t)(s.row0 + t0 + tok - base) * (kind ? v : k).row_stride + head * (kind ? v : k).head_stride + ch, wide >> kind & 1);
         bool nan = false;
 #pragma unroll
-        for (int m = 0; m < G / 32; ++m) {
-            x[m] = load_as_float(r.data, r.type, at + 32 * m);
+        for (int m = 0; m < 8; ++m) {
             nan |= isnan(x[m]);
             x[m] = fminf(fmaxf(x[m], -61440.f), 61440.f);
             low = fminf(low, x[m]);
             high = fmaxf(high, x[m]);
         }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
+        for (int d = G / 16; d; d >>= 1) {
             low = fminf(low, __shfl_xor_sync(~0u, low, d));
             high = fmaxf(high, __shfl_xor_sync(~0u, high, d));
+            nan |= (bool)__shfl_xor_sync(~0u, (int)nan, d);
         }
-        nan = __any_sync(~0u, nan);
         __half hs = __float2half_rn(__double2float_rn(((double)high - (double)low) / 15.0)), hm = __float2half_rn(low);
         if (nan) hs = hm = __float2half_rn(CUDART_NAN_F);
         const float sc = __half2float(hs), m0 = __half2float(hm), inv = 1.0f / sc;
+        unsigned q[8] = {};
+        if (sc > 0)
 #pragma unroll
-        for (int m = 0; m < G / 32; ++m) {
-            int q = 0;
-            if (sc > 0) {
+            for (int m = 0; m < 8; ++m) {
                 // the quotient in 32 bits is off by a few parts in 2^22 of at most 15 (or far above 15.5, where the code is 15 either
                 // way); only next to a border of two codes does that matter, and there it is made in 64 bits
                 const float a = (x[m] - m0) * inv, n = rintf(a);
-                q = (int)fminf(fmaxf(n, 0.f), 15.f);
-                if (fabsf(a - n) > 0.499f && a < 16.f) q = (int)fmin(fmax(rint(((double)x[m] - (double)m0) / (double)sc), 0.0), 15.0);
+                q[m] = (unsigned)fminf(fmaxf(n, 0.f), 15.f);
+                if (fabsf(a - n) > 0.499f && a < 16.f) q[m] = (unsigned)fmin(fmax(rint(((double)x[m] - (double)m0) / (double)sc), 0.0), 15.0);
             }
-            code[kind][tok][e * G + 32 * m + lane] = (unsigned char)q;
+        if (!here) continue;
+        if (kind == 0) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) word |= q[m] << (4 * m);
+            reinterpret_cast<uint32_t*>(image)[tok / 8 + 2 * (ch / 32 % 2) + 4 * (ch / 8 % 4) + 16 * (tok % 8) + 128 * (ch / 64)] = word;
+        } else {
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                code[8 * (ch / 16 % 4 + 4 * (tok / 2 % 4) + 16 * m + 128 * (ch / 64)) + ch / 8 % 2 + 2 * (tok / 8) + 4 * (tok % 2)] = (unsigned char)q[m];
         }
-        if (lane == 0) {
-            if (kind == 0) {
-                __half* p = reinterpret_cast<__half*>(out + S::K_PAR) + 2 * (e + S::E * (tok / 8 + 2 * (tok % 8)));
-                p[0] = hs;
-                p[1] = hm;
-            } else {
-                __half* p = reinterpret_cast<__half*>(out + S::V_PAR) + (tok % 2 + 2 * (tok / 8) + 8 * (tok / 2 % 4) + 32 * e);
-                p[0] = hs;
-                p[4] = hm;
-            }
+        if (ch % G == 0) {
+            __half* p = reinterpret_cast<__half*>(image + (kind ? S::V_PAR : S::K_PAR)) + (kind ? tok % 2 + 2 * (tok / 8) + 8 * (tok / 2 % 4) + 32 * e : 2 * (e + S::E * (tok / 8 + 2 * (tok % 8))));
+            p[0] = hs;
+            p[kind ? 4 : 1] = hm;
         }
     }
     __syncthreads();
+    if (from == 0 && to == 16) {
+        for (int w = threadIdx.x; w < 2 * D; w += IO_THREADS) reinterpret_cast<uint32_t*>(image + S::V_CODE)[w] = nibbles_of(reinterpret_cast<const uint2*>(code)[w]);
+        __syncthreads();
+        for (int w = threadIdx.x; w < S::BYTES / 16; w += IO_THREADS) reinterpret_cast<uint4*>(out)[w] = reinterpret_cast<const uint4*>(image)[w];
+        return;
+    }
+    // in part: the words and parameters of the tokens that are new; a value word keeps the others' nibbles
     for (int w = threadIdx.x; w < 2 * D; w += IO_THREADS) {
-        // key word w: eight channels of one token
-        const int tok = (w >> 4 & 7) + 8 * (w & 1), ch = 64 * (w >> 7) + 32 * (w >> 1 & 1) + 8 * (w >> 2 & 3);
-        if (tok >= from && tok < to) {
-            uint32_t word = 0;
-#pragma unroll
-            for (int b = 0; b < 8; ++b) word |= (uint32_t)code[0][tok][ch + b] << (4 * b);
-            reinterpret_cast<uint32_t*>(out)[w] = word;
-        }
-        // value word w: tokens 2j, 2j+1, 2j+8, 2j+9 of channels c and c+8
-        const int c0 = 16 * (w & 3) + 64 * (w >> 7) + (w >> 4 & 7), j = w >> 2 & 3;
-        uint32_t word = 0, mask = 0;
+        const int tok = (w >> 4 & 7) + 8 * (w & 1);
+        if (tok >= from && tok < to) reinterpret_cast<uint32_t*>(out)[w] = reinterpret_cast<const uint32_t*>(image)[w];
+        const int j = w >> 2 & 3;
+        uint32_t mask = 0;
 #pragma unroll
         for (int b = 0; b < 8; ++b) {
             const int u = 2 * j + 8 * (b >> 1 & 1) + (b >> 2);
-            if (u >= from && u < to) {
-                word |= (uint32_t)code[1][u][c0 + 8 * (b & 1)] << (4 * b);
-                mask |= 15u << (4 * b);
-            }
+            if (u >= from && u < to) mask |= 15u << (4 * b);
         }
         uint32_t* p = reinterpret_cast<uint32_t*>(out + S::V_CODE) + w;
-        if (mask) *p = mask == ~0u ? word : (*p & ~mask) | word;
+        if (mask) *p = (*p & ~mask) | (nibbles_of(reinterpret_cast<const uint2*>(code)[w]) & mask);
+    }
+    for (int w = threadIdx.x; w < 16 * S::E; w += IO_THREADS) {
+        const int kt = w / S::E % 2 * 8 + w / (2 * S::E);                    // key pair w: (scale, low)
+        if (kt >= from && kt < to) reinterpret_cast<uint32_t*>(out + S::K_PAR)[w] = reinterpret_cast<const uint32_t*>(image + S::K_PAR)[w];
+    }
+    for (int w = threadIdx.x; w < 32 * S::E; w += IO_THREADS) {
+        const int vt = 2 * (w >> 3 & 3) + (w & 1) + (w >> 1 & 1) * 8;        // value parameter w, scale or low
+        if (vt >= from && vt < to) reinterpret_cast<__half*>(out + S::V_PAR)[w] = reinterpret_cast<const __half*>(image + S::V_PAR)[w];
     }
 }
 
-template <int D, int G> __device__ __forceinline__ float key_at(const unsigned char* sub, int u, int ch) {
-    using S = Sub<D, G>;
-    const int nib = ch % 8 + 8 * (u / 8 + 2 * (ch / 32 % 2 + 2 * (ch / 8 % 4 + 4 * (u % 8 + 8 * (ch / 64)))));
-    const __half2 p = reinterpret_cast<const __half2*>(sub + S::K_PAR)[ch / G + S::E * (u / 8 + 2 * (u % 8))];
-    return fmaf(__low2float(p), (float)(sub[nib / 2] >> (4 * (nib % 2)) & 15), __high2float(p));
-}
-template <int D, int G> __device__ __forceinline__ float value_at(const unsigned char* sub, int u, int ch) {
-    using S = Sub<D, G>;
-    const int nib = ch / 8 % 2 + 2 * (u / 8) + 4 * (u % 2) + 8 * (ch / 16 % 4 + 4 * (u / 2 % 4 + 4 * (ch % 8 + 8 * (ch / 64))));
-    const __half* p = reinterpret_cast<const __half*>(sub + S::V_PAR) + (u % 2 + 2 * (u / 8) + 8 * (u / 2 % 4) + 32 * (ch / G));
-    return fmaf(__half2float(p[0]), (float)(sub[S::V_CODE + nib / 2] >> (4 * (nib % 2)) & 15), __half2float(p[4]));
-}
-
-// One block a (sub-block, head): the sub-block by way of shared memory, its tokens out in rows.
 template <int D, int G>
 __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned layer, List l, const int* first, unsigned subs, bf_rows k, bf_rows v,
-                                                          int* status) {
+                                                          int wide, int* status) {
     using S = Sub<D, G>;
+    constexpr int LANES = D / 8, UNITS = IO_THREADS / LANES;
     __shared__ __align__(16) unsigned char in[S::BYTES];
     const unsigned i = blockIdx.x / subs, head = blockIdx.y;
     const Span s = span_of(c, l, i);
@@ -178,11 +228,25 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
                                                       (t0 % c.page_tokens) / 16 * S::BYTES);
     for (int w = threadIdx.x; w < S::BYTES / 16; w += IO_THREADS) reinterpret_cast<uint4*>(in)[w] = src[w];
     __syncthreads();
-    for (int u = threadIdx.x; u < (to - from) * D; u += IO_THREADS) {
-        const int tok = from + u / D, ch = u % D;
-        const int64_t row = s.row0 + t0 + tok - base;
-        store_from_float(k.data, k.type, row * k.row_stride + head * k.head_stride + ch, key_at<D, G>(in, tok, ch));
-        store_from_float(v.data, v.type, row * v.row_stride + head * v.head_stride + ch, value_at<D, G>(in, tok, ch));
+    const int ch = (int)threadIdx.x % LANES * 8, unit = (int)threadIdx.x / LANES, e = ch / G;
+#pragma unroll 4
+    for (int u = 2 * from + unit; u < 2 * to; u += UNITS) {
+        const int kind = u & 1, tok = u >> 1;
+        float x[8];
+        if (kind == 0) {
+            const uint32_t word = reinterpret_cast<const uint32_t*>(in)[tok / 8 + 2 * (ch / 32 % 2) + 4 * (ch / 8 % 4) + 16 * (tok % 8) + 128 * (ch / 64)];
+            const __half2 p = reinterpret_cast<const __half2*>(in + S::K_PAR)[e + S::E * (tok / 8 + 2 * (tok % 8))];
+#pragma unroll
+            for (int m = 0; m < 8; ++m) x[m] = fmaf(__low2float(p), (float)(word >> (4 * m) & 15), __high2float(p));
+        } else {
+            const __half* p = reinterpret_cast<const __half*>(in + S::V_PAR) + (tok % 2 + 2 * (tok / 8) + 8 * (tok / 2 % 4) + 32 * e);
+            const float sc = __half2float(p[0]), lo = __half2float(p[4]);
+            const int nib = ch / 8 % 2 + 2 * (tok / 8) + 4 * (tok % 2), w0 = ch / 16 % 4 + 4 * (tok / 2 % 4) + 128 * (ch / 64);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) x[m] = fmaf(sc, (float)(reinterpret_cast<const uint32_t*>(in + S::V_CODE)[w0 + 16 * m] >> (4 * nib) & 15), lo);
+        }
+        const bf_rows& r = kind ? v : k;
+        store8(x, r, (int64_t)(s.row0 + t0 + tok - base) * r.row_stride + head * r.head_stride + ch, wide >> kind & 1);
     }
 }
 
@@ -850,9 +914,10 @@ extern "C" int bf_kv4_append(bf_trusted* t, const bf_kv4_cache* c, uint32_t laye
     ON_DEVICE(t);
     const List l{seqs, starts, n, max_new};
     const unsigned subs = subs_of(max_new);
+    const int wide = rows_wide(k, true) | rows_wide(v, true) << 1;
     with_shape(c, [&](auto s) {
         using S = decltype(s);
-        append_kernel<S::DIM, S::GROUP><<<dim3(n * subs, c->n_kv_heads), IO_THREADS, 0, t->stream>>>(cache, layer, l, subs, *k, *v, t->status);
+        append_kernel<S::DIM, S::GROUP><<<dim3(n * subs, c->n_kv_heads), IO_THREADS, 0, t->stream>>>(cache, layer, l, subs, *k, *v, wide, t->status);
     });
     return launched(t, "append_kernel");
 }
@@ -864,9 +929,10 @@ extern "C" int bf_kv4_read(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer,
     ON_DEVICE(t);
     const List l{seqs, starts, n, max_tokens};
     const unsigned subs = subs_of(max_tokens);
+    const int wide = rows_wide(k, true) | rows_wide(v, true) << 1;
     with_shape(c, [&](auto s) {
         using S = decltype(s);
-        read_kernel<S::DIM, S::GROUP><<<dim3(n * subs, c->n_kv_heads), IO_THREADS, 0, t->stream>>>(cache, layer, l, first, subs, *k, *v, t->status);
+        read_kernel<S::DIM, S::GROUP><<<dim3(n * subs, c->n_kv_heads), IO_THREADS, 0, t->stream>>>(cache, layer, l, first, subs, *k, *v, wide, t->status);
     });
     return launched(t, "read_kernel");
 }
