@@ -357,7 +357,7 @@ typedef struct {
 
 /* y[i] = W x[i] for n rows: the plaintext counterpart of bf_linear, for projections that stay in the trusted domain (the
  * vocabulary).  Products are of the 4-bit codes themselves, sums in 32 bits, one rounding to the type of y.  x may be any type,
- * y another.  A non-finite x makes its row of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, CUDA. */
+ * y another.  A non-finite x makes its row of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
 int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y);
 
 /* The encrypted product from the same matrix, on the accelerator (weights are public to it): bf_encode_weights_split and bf_linear with

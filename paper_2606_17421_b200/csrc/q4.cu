@@ -625,9 +625,13 @@ template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_r
     p.segs = segs;
     const uint64_t all = (uint64_t)n * per_row;
     p.width = all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : 64;
-    p.seg_bytes = p.width * (512 + SEG / G * 4);
-    p.chunk_bytes = p.seg_bytes * segs;
-    uint64_t chunks = t->ws_bytes / (p.chunk_bytes + p.width * 4 + 256);
+    uint64_t chunks = 0;
+    for (;; p.width /= 2) {                                      // (narrower where the workspace does not hold one chunk)
+        p.seg_bytes = p.width * (512 + SEG / G * 4);
+        p.chunk_bytes = p.seg_bytes * segs;
+        chunks = t->ws_bytes / (p.chunk_bytes + p.width * 4 + 256);
+        if (chunks || p.width == 8) break;
+    }
     if (chunks == 0) return BF_ERR_TOO_LARGE;
     if (chunks > 1024) chunks = 1024;
     const unsigned rows_at_once = (unsigned)(chunks * p.width / per_row);

@@ -918,3 +918,99 @@ def test_attention_keeps_a_nan_to_the_rows_that_see_it(side):
             sub[:] = keep
             assert np.isnan(bad[sees]).all() and np.array_equal(bad[~sees], clean[~sees])
     assert status_of(side) == 0
+
+
+@gpu
+def test_cache_calls_on_rows_without_alignment(side):
+    """Rows that start anywhere and lie any distance apart: element by element, the same bytes and results."""
+    torch = side.torch
+    c = ref.Cache(1, 8, 2, 64, 32, 16, 2, 4)
+    lens = [50, 33]
+    for type in ("bf16", "fp32"):
+        d, e = DeviceCache(side, c), DeviceCache(side, c)
+        flat = torch.randn(83 * 4 * 67 + 1, device="cuda").to(side.types[type])
+        odd = flat[1:].view(83, 4, 67)[:, :, :64]
+        even = odd.contiguous()
+        st, cs = side.ints([0, 50, 83]), side.ints(lens)
+        for cache, x in ((d, odd), (e, even)):
+            bf.bf_kv4_grow(side.t, cache.desc, None, cs, 2)
+            bf.bf_kv4_append(side.t, cache.desc, 0, None, st, 2, 50, bf.bf_rows.of(x[:, :2]), bf.bf_rows.of(x[:, 2:]))
+        assert np.array_equal(side.host(d.pool), side.host(e.pool))
+        out = torch.zeros_like(flat)[1:].view(83, 4, 67)[:, :, :64]
+        bf.bf_kv4_read(side.t, d.desc, 0, None, st, None, 2, 50, bf.bf_rows.of(out[:, :2]), bf.bf_rows.of(out[:, 2:]))
+        flush = torch.zeros_like(even)
+        bf.bf_kv4_read(side.t, d.desc, 0, None, st, None, 2, 50, bf.bf_rows.of(flush[:, :2]), bf.bf_rows.of(flush[:, 2:]))
+        assert torch.equal(out, flush) and bool((out != 0).any())
+        if type == "fp32":
+            continue
+        res, flush = torch.zeros_like(flat)[1:].view(83, 4, 67)[:, :, :64], torch.zeros_like(even)
+        for x, o in ((odd, res), (even, flush)):
+            bf.bf_kv4_attention(side.t, d.desc, 0, None, st, 2, 50, 50, bf.bf_rows.of(x), 4, bf.bf_rows.of(o), 0.125)
+        assert torch.equal(res, flush)
+    assert status_of(side) == 0
+
+
+@gpu
+def test_small_workspace(side):
+    """A context with the least workspace: the same results in smaller portions, or a refusal that enqueues nothing."""
+    torch = side.torch
+    t = bf.bf_trusted_create(1 << 20, side.stream.cuda_stream)
+    try:
+        rng = np.random.default_rng(1)
+        for n, d_in in ((150, 700), (40, 6000), (3, 20000)):
+            packed, scales, _, _, _ = draw_matrix(rng, 33, d_in, 128, False)
+            codes, sc = side.dev(packed), side.dev(scales)
+            M = bf.bf_q4_matrix.of(codes, sc, None, d_in, 128)
+            x = torch.randn((n, d_in), device="cuda").bfloat16()
+            y, z = torch.zeros((n, 33), device="cuda"), torch.ones((n, 33), device="cuda")
+            bf.bf_q4_linear(side.t, M, bf.bf_rows.of(x), n, bf.bf_rows.of(y))
+            bf.bf_q4_linear(t, M, bf.bf_rows.of(x), n, bf.bf_rows.of(z))
+            assert np.abs(side.host(y) - side.host(z)).max() <= 2.0 ** -18 * np.abs(side.host(y)).max()
+        packed, scales, _, _, _ = draw_matrix(rng, 2, 70000, 128, False)
+        codes, sc = side.dev(packed), side.dev(scales)
+        x, y = torch.randn((2, 70000), device="cuda"), torch.full((2, 2), 3.0, device="cuda")
+        refused(bf.BF_ERR_TOO_LARGE, bf.bf_q4_linear, t, bf.bf_q4_matrix.of(codes, sc, None, 70000, 128), bf.bf_rows.of(x), 2, bf.bf_rows.of(y))
+        assert (side.host(y) == 3).all()
+        c = ref.Cache(1, 300, 1, 64, 64, 16, 2, 150)
+        d = fill(side, c, [2000, 1500])
+        q = torch.randn((2, 8, 64), device="cuda").half()
+        check_attention(side, d, 0, None, [1, 1], q, 8, 0, "fp16", starts_given=False)
+        o = torch.zeros_like(q)
+        bf.bf_kv4_attention(t, d.desc, 0, None, None, 2, 1, 2000, bf.bf_rows.of(q), 8, bf.bf_rows.of(o), 0.125)
+        p = torch.zeros_like(q)
+        bf.bf_kv4_attention(side.t, d.desc, 0, None, None, 2, 1, 2000, bf.bf_rows.of(q), 8, bf.bf_rows.of(p), 0.125)
+        assert (side.host(o) - side.host(p)).__abs__().max() <= 2.0 ** -9 * np.abs(side.host(p)).max()
+    finally:
+        bf.bf_trusted_destroy(t)
+
+
+@gpu
+def test_layers_beyond_32_bits_of_offset(side):
+    """A layer's pages behind 4 GB of the pool: copies, writes, attention and compaction reach them."""
+    torch = side.torch
+    T, heads, pages, layers = 256, 8, 40000, 2
+    block = bf.bf_kv4_block_bytes(128, 128, T)
+    if torch.cuda.mem_get_info()[0] < 3 * layers * pages * heads * block // 2:
+        pytest.skip("not enough memory")
+    pool = torch.empty((layers, pages, heads, block), dtype=torch.uint8, device="cuda")
+    assert pool[0].numel() > 2 ** 33
+    tables, lengths, refs = side.ints([[pages - 1, 0], [-1, -1]]), side.ints([300, 0]), torch.zeros(pages, dtype=torch.int32, device="cuda")
+    refs[0] = refs[pages - 1] = 1
+    cache = bf.bf_kv4_cache.of(pool, tables, lengths, refs, 128, 128, T)
+    k, v = (torch.randn((300, heads, 128), device="cuda").half() for _ in range(2))
+    st = side.ints([0, 300])
+    bf.bf_kv4_append(side.t, cache, 1, None, st, 1, 300, bf.bf_rows.of(k), bf.bf_rows.of(v))
+    q = torch.randn((1, heads, 128), device="cuda").half()
+    a, b, kk, vv = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    bf.bf_kv4_attention(side.t, cache, 1, None, None, 1, 1, 300, bf.bf_rows.of(q), heads, bf.bf_rows.of(a), 0.1)
+    bf.bf_kv4_fork(side.t, cache, src := side.ints([0]), dst := side.ints([1]), 1)
+    bf.bf_kv4_free(side.t, cache, src, 1)
+    bf.bf_kv4_compact(side.t, cache)
+    bf.bf_kv4_attention(side.t, cache, 1, dst, None, 1, 1, 300, bf.bf_rows.of(q), heads, bf.bf_rows.of(b), 0.1)
+    bf.bf_kv4_read(side.t, cache, 1, dst, st, None, 1, 300, bf.bf_rows.of(kk), bf.bf_rows.of(vv))
+    assert status_of(side) == 0 and side.host(tables).tolist() == [[-1, -1], [0, 1]]
+    assert torch.equal(a, b)
+    # half a step of the codes, and what rounding low and scale moves (2^-11 of each, the scale up to 15 times)
+    for x, held in ((k, kk), (v, vv)):
+        span = (x.float().amax(-1, keepdim=True) - x.float().amin(-1, keepdim=True))
+        assert bool(((x.float() - held.float()).abs() <= span / 30 + 2.0 ** -10 * (span + x.float().abs().amax(-1, keepdim=True)) + 2.0 ** -11 * held.float().abs()).all())
