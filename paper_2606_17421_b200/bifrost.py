@@ -7,6 +7,7 @@ memory and streams.  There is no fallback: if the CUDA library has not been buil
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -41,16 +42,19 @@ BF_F16 = 1
 BF_BF16 = 2
 
 
-def _type_of(tensor) -> int:
-    name = str(tensor.dtype)
-    types = {"torch.float32": BF_F32, "torch.float16": BF_F16, "torch.bfloat16": BF_BF16}
-    if name not in types:
-        raise ValueError(f"rows are float32, float16 or bfloat16, not {name}")
-    return types[name]
+_ROW_TYPES = {"torch.float32": BF_F32, "torch.float16": BF_F16, "torch.bfloat16": BF_BF16}
+_NAMES = {}                       # torch dtype -> its name, which is slow to make
+
+
+def _name(dtype) -> str:
+    name = _NAMES.get(dtype)
+    if name is None:
+        name = _NAMES[dtype] = str(dtype)
+    return name
 
 
 def _dense(tensor, dtype: str, what: str):
-    if str(tensor.dtype) != dtype or not tensor.is_contiguous():
+    if _name(tensor.dtype) != dtype or not tensor.is_contiguous():
         raise ValueError(f"{what}: a contiguous {dtype} tensor is wanted")
     return tensor.data_ptr()
 
@@ -61,9 +65,13 @@ class bf_rows(ctypes.Structure):
     @classmethod
     def of(cls, tensor):
         """Rows [n][channels] or [n][heads][channels] of a tensor, which must live as long; any strides but the channels'."""
-        if tensor.dim() not in (2, 3) or (tensor.stride(-1) != 1 and tensor.shape[-1] != 1):
+        strides, kind = tensor.stride(), _ROW_TYPES.get(_name(tensor.dtype))
+        dims = len(strides)
+        if (dims != 3 and dims != 2) or (strides[-1] != 1 and tensor.shape[-1] != 1):
             raise ValueError("rows are [n][channels] or [n][heads][channels] with the channels side by side")
-        return cls(tensor.data_ptr(), tensor.stride(0), tensor.stride(1) if tensor.dim() == 3 else 0, _type_of(tensor))
+        if kind is None:
+            raise ValueError(f"rows are float32, float16 or bfloat16, not {tensor.dtype}")
+        return cls(tensor.data_ptr(), strides[0], strides[1] if dims == 3 else 0, kind)
 
 
 class bf_q4_matrix(ctypes.Structure):
@@ -73,13 +81,13 @@ class bf_q4_matrix(ctypes.Structure):
     @classmethod
     def of(cls, codes, scales, offsets, d_in: int, group: int):
         """codes uint8 [d_out][row_bytes], scales (and offsets, or None) float16 [d_out][group_stride]; they must live as long."""
-        if offsets is not None and offsets.shape != scales.shape:
+        c, s = codes.shape, scales.shape
+        if offsets is not None and offsets.shape != s:
             raise ValueError("offsets have the shape of the scales")
-        if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
+        if len(c) != 2 or len(s) != 2 or c[0] != s[0]:
             raise ValueError("codes and scales have a row for each output")
         return cls(_dense(codes, "torch.uint8", "codes"), _dense(scales, "torch.float16", "scales"),
-                   None if offsets is None else _dense(offsets, "torch.float16", "offsets"), codes.shape[1], scales.shape[1], codes.shape[0],
-                   d_in, group)
+                   None if offsets is None else _dense(offsets, "torch.float16", "offsets"), c[1], s[1], c[0], d_in, group)
 
 
 class bf_kv4_cache(ctypes.Structure):
@@ -93,10 +101,11 @@ class bf_kv4_cache(ctypes.Structure):
         layers, pages, heads, block = pool.shape
         if block != bf_kv4_block_bytes(head_dim, group, page_tokens):
             raise BifrostError(BF_ERR_SHAPE, "bf_kv4_cache", f"a block of {block} bytes")
-        if tables.dim() != 2 or lengths.shape != tables.shape[:1] or refs.shape != pool.shape[1:2]:
+        seqs, n_seqs, n_refs = tables.shape, lengths.shape, refs.shape
+        if len(seqs) != 2 or len(n_seqs) != 1 or len(n_refs) != 1 or n_seqs[0] != seqs[0] or n_refs[0] != pages:
             raise BifrostError(BF_ERR_SHAPE, "bf_kv4_cache", "tables, lengths and refs do not fit together")
         return cls(_dense(pool, "torch.uint8", "pool"), _dense(tables, "torch.int32", "tables"), _dense(lengths, "torch.int32", "lengths"),
-                   _dense(refs, "torch.int32", "refs"), layers, pages, heads, head_dim, group, page_tokens, tables.shape[0], tables.shape[1])
+                   _dense(refs, "torch.int32", "refs"), layers, pages, heads, head_dim, group, page_tokens, seqs[0], seqs[1])
 
 
 class BifrostError(RuntimeError):
@@ -445,6 +454,7 @@ def bf_linear_q4(ctx, ct_in, n_in: int, W: bf_q4_matrix, ct_out, n_out: int):
     _check(load().bf_linear_q4(ctx, _ptr(ct_in), n_in, _ref(W), _ptr(ct_out), n_out), "bf_linear_q4", ctx)
 
 
+@functools.lru_cache(None)
 def bf_kv4_block_bytes(head_dim: int, group: int, page_tokens: int) -> int:
     return load().bf_kv4_block_bytes(head_dim, group, page_tokens)
 

@@ -4,6 +4,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <cstdio>
 
@@ -46,6 +47,16 @@ inline int cuda_failed(bf_trusted* t, const char* what, cudaError_t e) {
 inline int launched(bf_trusted* t, const char* what) {
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BF_OK : cuda_failed(t, what, e);
+}
+
+// Dynamic shared memory that a kernel may ask for: set once a device, since the call costs as much as a third of a launch.
+template <auto KERNEL> cudaError_t room_for(const bf_trusted* t, size_t bytes) {
+    static std::atomic<unsigned long long> done{0};
+    const unsigned long long bit = t->device >= 0 && t->device < 64 ? 1ull << t->device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 inline bool type_ok(int32_t type) { return type == BF_F32 || type == BF_F16 || type == BF_BF16; }

@@ -877,7 +877,7 @@ template <int D, int G, int NT> int attention(bf_trusted* t, Att p, unsigned n, 
     constexpr size_t ring = (size_t)ATT_WARPS * ATT_STAGES * S::BYTES, red = (size_t)ATT_WARPS * 8 * (D + 4) * 4;
     constexpr size_t first = (D / 32) * RW * 64 + (D / G) * RW * 4 + (ring > red ? ring : red), join = RW * MOST_SPLITS * 4 + ATT_WARPS * 32 * 16;
     constexpr size_t smem = first > join ? first : join;
-    const cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, G, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = room_for<attention_kernel<D, G, NT>>(t, smem);
     if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
     attention_kernel<D, G, NT><<<(unsigned)(sets * splits), ATT_WARPS * 32, smem, t->stream>>>(p);
     return launched(t, "attention_kernel");

@@ -337,7 +337,7 @@ template <int G> FewPlan few_plan(const Q4& w, unsigned cols, unsigned n_sm) {
 
 template <int G, bool OFFSETS> int few_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned n, const bf_rows& y, unsigned cols) {
     const FewPlan p = few_plan<G>(w, cols, t->n_sm);
-    const cudaError_t e = cudaFuncSetAttribute(q4_few_kernel<G, OFFSETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    const cudaError_t e = room_for<q4_few_kernel<G, OFFSETS>>(t, SMEM_MAX);
     if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
     q4_few_kernel<G, OFFSETS><<<p.grid, p.warps * 32, p.smem, t->stream>>>(w, x, n, y, cols, p.kw, rows_wide(&x, false));
     return launched(t, "q4_few_kernel");
@@ -597,7 +597,7 @@ int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
     unsigned stages = 4;
     while (stages > 2 && stages * stage + red > (per_sm == 2 ? SMEM_MAX / 2 - 1024 : SMEM_MAX)) --stages;
     const unsigned per_block = MANY_WARPS / kw, blocks = (tiles + per_block - 1) / per_block, most_blocks = t->n_sm * per_sm;
-    cudaError_t e = cudaFuncSetAttribute(q4_many_kernel<G, OFFSETS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    cudaError_t e = room_for<q4_many_kernel<G, OFFSETS, NT>>(t, SMEM_MAX);
     if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks < most_blocks ? blocks : most_blocks, chunks);

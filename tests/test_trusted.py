@@ -176,10 +176,16 @@ class Side:
 
 
 @pytest.fixture(scope="module")
-def side():
+def one_side():
     s = Side()
     yield s
     bf.bf_trusted_destroy(s.t)
+
+
+@pytest.fixture
+def side(one_side):
+    one_side.torch.cuda.set_stream(one_side.stream)          # (a runner that a test made has set its own)
+    return one_side
 
 
 HALF_STEP = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
