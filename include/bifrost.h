@@ -39,7 +39,7 @@ enum {
     BF_ERR_CUDA = -7,          /* a CUDA call failed; see bf_last_cuda_error() */
     BF_ERR_RANGE = -8,         /* an encoded coefficient does not fit 2^62 (scale too large for the data) */
     BF_ERR_TOO_LARGE = -9,     /* more work than the fixed scratch of an allocation-free entry point holds */
-    BF_ERR_TIMEOUT = -10       /* reserved, not returned: no kernel waits on anything but the end of the one before it */
+    BF_ERR_TIMEOUT = -10       /* a wait of a kernel for its own matrix instructions gave up (bf_trusted_status; results are invalid) */
 };
 
 typedef struct bf_ctx bf_ctx;          /* ring tables, rotation keys, scratch memory */
@@ -325,7 +325,7 @@ typedef struct bf_trusted bf_trusted;  /* stream, status word, workspace */
  * needs more than there is returns BF_ERR_TOO_LARGE and enqueues nothing.  Allocates; synchronises.  Errors: INVALID_ARG, OOM, CUDA. */
 int bf_trusted_create(bf_trusted** out, uint64_t workspace_bytes, void* cuda_stream);
 void bf_trusted_destroy(bf_trusted* t);                       /* synchronises */
-/* Synchronises the stream, returns what the kernels found since the last call, and forgets it: BF_ERR_RANGE (an index or a
+/* Synchronises the stream, returns what the kernels found since the last call, and forgets it: BF_ERR_TIMEOUT, else BF_ERR_RANGE (an index or a
  * length in device memory was out of range, a list named a sequence twice where that has no meaning, a reference count went
  * below zero), else BF_ERR_OOM (the pool ran out of pages), else BF_OK.  INVALID_ARG while the stream is being captured. */
 int bf_trusted_status(bf_trusted* t);

@@ -212,7 +212,7 @@ extern "C" const char* bf_strerror(int code) {
         case BF_ERR_OOM: return "out of memory or over the cache budget";
         case BF_ERR_CUDA: return "CUDA error";
         case BF_ERR_RANGE: return "encoded coefficient out of range";
-        case BF_ERR_TIMEOUT: return "a device-side wait gave up (reserved: no kernel waits)";
+        case BF_ERR_TIMEOUT: return "a device-side wait gave up";
         case BF_ERR_TOO_LARGE: return "request exceeds the fixed capacity of the allocation-free entry point";
         default: return "unknown error";
     }

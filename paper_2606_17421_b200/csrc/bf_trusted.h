@@ -23,7 +23,7 @@ struct bf_trusted {
 
 namespace bft {
 
-constexpr int ST_RANGE = 1, ST_OOM = 2;         // bits of the status word
+constexpr int ST_RANGE = 1, ST_OOM = 2, ST_TIMEOUT = 4;         // bits of the status word
 constexpr unsigned ARRIVALS = 4096;
 
 // The context's device current for the length of a call.

@@ -86,11 +86,11 @@ __device__ __forceinline__ float warp_largest(float big) {
     return big;
 }
 
-// The same as operands, relative to `big`: a lane's 16 bytes at frag[(lane / 4 * cols + col) * 4 + lane % 4], the sums of the groups times
-// 2^-24 at sums[group * sums_step + col], and what undoes the scaling at undo[col] (from one lane where `tell`); fp32 fills two columns.
-template <int G>
-__device__ __forceinline__ void x_unit(float (&v)[8], float big, bool two, uint4* frag, float* sums, unsigned sums_step, float* undo, bool tell,
-                                       unsigned cols, unsigned col) {
+// The same as operands, relative to `big`: a lane's 16 bytes at *place(col), the sums of the groups times 2^-24 at sums[group * sums_step
+// + col], and what undoes the scaling at undo[col] (from one lane where `tell`); fp32 fills two columns.
+template <int G, typename Place>
+__device__ __forceinline__ void x_unit(float (&v)[8], float big, bool two, Place place, float* sums, unsigned sums_step, float* undo, bool tell,
+                                       unsigned col) {
     const unsigned lane = threadIdx.x & 31;
     // 2^k with 2^14 <= big 2^k < 2^15, where 2^k is a float
     const int e = max(1, (int)(__float_as_uint(big) >> 23));
@@ -111,7 +111,7 @@ __device__ __forceinline__ void x_unit(float (&v)[8], float big, bool two, uint4
         o.y = half2_bits(__half2float(h[1]) * q, __half2float(h[5]) * q);
         o.z = half2_bits(__half2float(h[2]), __half2float(h[6]));
         o.w = half2_bits(__half2float(h[3]) * q, __half2float(h[7]) * q);
-        frag[(lane / 4 * cols + col) * 4 + lane % 4] = o;
+        *place(col) = o;
 #pragma unroll
         for (int d = G / 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
         if (lane % (G / 8) == 0) sums[lane / (G / 8) * sums_step + col] = s * 0x1p-24f;
@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(MOST_WARPS * 32) q4_few_kernel(Q4 w, bf_rows x
         for (unsigned i = 0; i < X_AT_ONCE; ++i) {
             const unsigned seg = (u0 + i * warps) % segs, row = (u0 + i * warps) / segs;
             if (u0 + i * warps < segs * n)
-                x_unit<G>(v[i], warp_largest(largest(v[i])), two, frag + (size_t)seg * SEG_BLOCKS * cols * 4, sums + seg * GROUPS * 8, 8, undo + seg * 8,
-                          true, cols, two ? 2 * row : row);
+                x_unit<G>(v[i], warp_largest(largest(v[i])), two, [&](unsigned c) { return frag + (((size_t)seg * SEG_BLOCKS + lane / 4) * cols + c) * 4 + lane % 4; },
+                          sums + seg * GROUPS * 8, 8, undo + seg * 8, true, two ? 2 * row : row);
         }
     }
     __syncthreads();
@@ -349,6 +349,7 @@ struct Prepared {
     unsigned char* at;            // [column chunk][seg]: operands of `width` columns, then the sums of their groups
     float* undo;                  // [columns]
     unsigned width, segs;
+    bool tiled;                   // as q4_wide_kernel takes it
     size_t seg_bytes, chunk_bytes;
 };
 
@@ -379,8 +380,11 @@ __global__ void __launch_bounds__(PREP_WARPS * 32) q4_prepare_kernel(bf_rows x, 
     const unsigned col = two ? 2 * row : row, chunk = col / p.width;          // (a chunk's width is even)
     auto make = [&](float (&u)[8], unsigned seg) {
         unsigned char* at = p.at + chunk * p.chunk_bytes + seg * p.seg_bytes;
-        x_unit<G>(u, big, two, reinterpret_cast<uint4*>(at), reinterpret_cast<float*>(at + p.width * 512), p.width, p.undo + chunk * p.width, seg == 0,
-                  p.width, col % p.width);
+        const unsigned lane = threadIdx.x % 32;
+        x_unit<G>(u, big, two, [&](unsigned c) {
+            // rows of 128 bytes, 64 columns of x each, their 16-byte pieces exchanged by the row's number; or fragments side by side
+            return reinterpret_cast<uint4*>(at) + (p.tiled ? (lane / 8 * p.width + c) * 8 + (lane % 8 ^ c % 8) : (lane / 4 * p.width + c) * 4 + lane % 4);
+        }, reinterpret_cast<float*>(at + p.width * 512), p.width, p.undo + chunk * p.width, seg == 0, col % p.width);
     };
 #pragma unroll
     for (unsigned i = 0; i < PREP_HELD; ++i)
@@ -616,6 +620,273 @@ int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
 // Segments of x that every block makes operands of by itself; more are made once, which costs a launch.  4096 x 4096, 1 / 2 / 4 / 8 rows
 // (16 segments each): in every block 6.1 / 6.9 / 8.7 / 12.4 us, by a kernel of its own 6.7 / 6.7 / 6.7 / 6.7.
 constexpr unsigned FEW_UNITS = 32;
+// ------------------------------------------------------------------------------------------------
+// Many rows of W as well: the fifth-generation matrix instructions.  A block of 128 threads has 128 rows of W, a thread a row.  Codes go from
+// shared memory through registers (the same ANDs) to TMEM, 128 columns of W at a time, as operand A (K pairs in 32-bit columns, K in
+// the order in which a word unpacks); x is operand B in shared memory, rows of 128 bytes in the 128-byte swizzle; one thread issues
+// the products of a group of columns into its own accumulators, and each thread multiplies its row's sums by the group's scale.
+// While the products run, the next 128 columns are unpacked.  Waits are bounded; one that gives up is BF_ERR_TIMEOUT.
+constexpr unsigned TILE = 128;
+
+__device__ __forceinline__ bool wait_for(uint32_t bar, unsigned parity) {
+    for (int i = 0; i < (1 << 17); ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                 "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t (&r)[16], uint32_t at) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+}
+
+template <int G, bool OFFSETS, int N> struct Wide {
+    static constexpr unsigned GROUPS = SEG / G, PAR = GROUPS * 2, IN_UNIT = TILE / G;      // groups of a stage, of a unit of 128 columns
+    static constexpr unsigned X = N * 512, CODES = TILE * SEG / 2, PARS = TILE * PAR * (OFFSETS ? 2 : 1), SUMS = GROUPS * N * 4;
+    static constexpr unsigned STAGE = X + CODES + PARS;                      // (sums have a slot more: they are read for one stage longer)
+    static constexpr unsigned TMEM = 64 + IN_UNIT * N <= 128 ? 128 : 64 + IN_UNIT * N <= 256 ? 256 : 512;   // columns: A, then the sums
+};
+
+template <int G, bool OFFSETS, int N>
+__global__ void __launch_bounds__(TILE, N == 64 || Wide<G, OFFSETS, N>::TMEM > 128 ? 2 : TILE / G * N > 32 || N == 32 ? 3 : 4) q4_wide_kernel(Q4 w, Prepared p, unsigned cols, unsigned stages, bf_rows y, unsigned row0, int* status) {
+    using M = Wide<G, OFFSETS, N>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ __align__(8) unsigned long long bar_word;
+    __shared__ uint32_t tmem_word;
+    const unsigned warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = threadIdx.x;
+    const unsigned tiles = (w.d_out + TILE - 1) / TILE, steps = p.segs;
+    const uint32_t base = ((uint32_t)__cvta_generic_to_shared(smem) + 1023) & ~1023u;                   // operand B lies on 1024 bytes
+    unsigned char* at_base = smem + (base - (uint32_t)__cvta_generic_to_shared(smem));
+    const uint32_t codes_at = base + stages * M::X, pars_at = codes_at + stages * M::CODES, sums_at = pars_at + stages * M::PARS;
+    const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&bar_word);
+    const unsigned char* x_from = p.at + blockIdx.y * p.chunk_bytes;
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_word)), "n"(M::TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (threadIdx.x == 0) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+
+    // stages to bring in: a warp its own 32 rows of codes and parameters, all of them x
+    unsigned in_tile = blockIdx.x, in_step = 0, in_slot = 0, in_sums = 0;
+    const unsigned cr = lane / 8, cb = lane % 8;
+    auto fetch_weights = [&]() {
+        if (in_tile >= tiles) return;
+        const unsigned r0 = in_tile * TILE + warp * 32;
+        const uint32_t to = codes_at + in_slot * M::CODES + warp * 32 * 128;
+        const size_t at = (size_t)in_step * (SEG / 2) + cb * 16;
+        const uint8_t* from = w.codes + (size_t)(r0 + cr) * w.row_bytes + at;
+        if (r0 + 32 <= w.d_out && (size_t)(in_step + 1) * (SEG / 2) <= w.row_bytes) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) copy16(to + (cr + 4 * i) * 128 + ((cb ^ ((cr + 4 * i) & 7)) * 16), from + (size_t)(4 * i) * w.row_bytes);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool some = at < w.row_bytes && r0 + cr + 4 * i < w.d_out;
+                copy16(to + (cr + 4 * i) * 128 + ((cb ^ ((cr + 4 * i) & 7)) * 16), some ? from + (size_t)(4 * i) * w.row_bytes : w.codes, some);
+            }
+        }
+        const size_t par = (size_t)min(in_tile * TILE + row, w.d_out - 1) * w.group_stride + in_step * M::GROUPS;
+        copy_par<M::PAR>(pars_at + in_slot * M::PARS + row * M::PAR, w.scales + par);
+        if (OFFSETS) copy_par<M::PAR>(pars_at + in_slot * M::PARS + (TILE + row) * M::PAR, w.offsets + par);
+    };
+    auto step_on = [&]() {
+        in_slot = in_slot + 1 == stages ? 0 : in_slot + 1;
+        if (++in_step == steps) in_step = 0, in_tile += gridDim.x;
+    };
+    auto fetch_x = [&]() {
+        if (in_tile < tiles) {
+            const unsigned char* from = x_from + (size_t)in_step * (M::X + M::SUMS);
+            for (unsigned o = threadIdx.x * 16; o < M::X; o += TILE * 16) copy16(base + in_slot * M::X + o, from + o);
+            for (unsigned o = threadIdx.x * 16; o < M::SUMS; o += TILE * 16) copy16(sums_at + in_sums * M::SUMS + o, from + M::X + o);
+        }
+        asm volatile("cp.async.commit_group;");
+        in_sums = in_sums == stages ? 0 : in_sums + 1;
+        step_on();
+    };
+    for (unsigned i = 0; i + 1 < stages; ++i) {
+        fetch_weights();
+        step_on();
+    }
+    in_tile = blockIdx.x, in_step = in_slot = 0;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (unsigned i = 0; i + 1 < stages; ++i) fetch_x();
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_word, mine = tmem + (warp * 32 << 16);        // this warp's 32 lanes of it
+    // f16 operands, both K-major, f32 sums, 128 x N; operand B: 128-byte swizzle, 1024 bytes from 8 rows to the next
+    constexpr uint32_t IDESC = 1u << 4 | (N / 8) << 17 | (TILE / 16) << 24;
+    constexpr unsigned long long BDESC = 2ull << 61 | 1ull << 46 | (1024ull >> 4) << 32 | 1ull << 16;
+
+    bool dead = false;
+    unsigned slot = 0, sums_slot = 0, parity = 0;
+    for (unsigned tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        float total[N] = {};
+        // the sums of a unit: of the groups of columns whose scales are s (and z), times what x was summed to
+        uint32_t acc[M::IN_UNIT][N / 16][16];
+        Pars<M::GROUPS> s, z, s_old, z_old;
+        unsigned old_sums = 0, old_unit = 0, old_groups = 0;
+        auto take = [&]() {                                      // (what was loaded before)
+            const float* xs = reinterpret_cast<const float*>(at_base + (sums_at - base) + old_sums * M::SUMS) + old_unit * M::IN_UNIT * N;
+#pragma unroll
+            for (int e = 0; e < (int)M::IN_UNIT; ++e) {
+                const int ge = old_unit * M::IN_UNIT + e;
+                const float f = ge < (int)old_groups ? s_old.get(old_unit ? M::IN_UNIT + e : e) : 0.f;
+                const float h = ge < (int)old_groups ? (OFFSETS ? z_old.get(old_unit ? M::IN_UNIT + e : e) : 0.f) - 8.f * f : 0.f;
+#pragma unroll
+                for (int c = 0; c < N; c += 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(xs + e * N + c);
+                    total[c] += f * __uint_as_float(acc[e][c / 16][c % 16]) + h * v.x;
+                    total[c + 1] += f * __uint_as_float(acc[e][c / 16][c % 16 + 1]) + h * v.y;
+                    total[c + 2] += f * __uint_as_float(acc[e][c / 16][c % 16 + 2]) + h * v.z;
+                    total[c + 3] += f * __uint_as_float(acc[e][c / 16][c % 16 + 3]) + h * v.w;
+                }
+            }
+        };
+        auto load_sums = [&]() {
+#pragma unroll
+            for (int e = 0; e < (int)M::IN_UNIT; ++e)
+#pragma unroll
+                for (int c = 0; c < N / 16; ++c) tmem_load16(acc[e][c], mine + 64 + e * N + c * 16);
+        };
+        for (unsigned step = 0; step < steps; ++step) {
+            if (stages == 3) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // x, for the matrix instructions
+            __syncwarp();
+            const unsigned char* st = at_base + (codes_at - base) + slot * M::CODES + row * 128;
+            const unsigned char* pr = at_base + (pars_at - base) + slot * M::PARS + row * M::PAR;
+            s.load(pr);
+            if (OFFSETS) z.load(pr + TILE * M::PAR);
+            const unsigned groups = (w.d_in - step * SEG + G - 1) / G;
+#pragma unroll
+            for (unsigned unit = 0; unit < 2; ++unit) {
+                uint32_t a[64];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(st + (((unit * 4 + c) ^ (row & 7)) * 16));
+                    const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t u = word[k], h = u >> 8;
+                        a[c * 16 + k * 4] = u & 0x000f000fu, a[c * 16 + k * 4 + 1] = u & 0x00f000f0u;
+                        a[c * 16 + k * 4 + 2] = h & 0x000f000fu, a[c * 16 + k * 4 + 3] = h & 0x00f000f0u;
+                    }
+                }
+                const bool before = step || unit;                // products are under way: their end, their sums
+                if (before) {
+                    if (!dead && !wait_for(bar, parity)) dead = true;
+                    parity ^= 1;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    load_sums();
+                }
+                tmem_store32(mine, a);
+                tmem_store32(mine + 32, a + 32);
+                if (before) asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t b_at = base + slot * M::X + unit * 2 * (N * 128);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const unsigned long long desc = BDESC | ((b_at + k / 4 * (N * 128) + k % 4 * 32) >> 4 & 0x3fff);
+                        const uint32_t more = k % (G / 16) != 0;
+                        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                                     ::"r"(tmem + 64 + k / (G / 16) * N), "r"(tmem + k * 8), "l"(desc), "r"(IDESC), "r"(more) : "memory");
+                    }
+                    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+                }
+                __syncwarp();
+                if (unit == 0) {                                 // the stage before this one is free
+                    fetch_weights();
+                    fetch_x();
+                }
+                if (before) take();
+                s_old = s;
+                if (OFFSETS) z_old = z;
+                old_sums = sums_slot, old_unit = unit, old_groups = groups;
+            }
+            slot = slot + 1 == stages ? 0 : slot + 1;
+            sums_slot = sums_slot == stages ? 0 : sums_slot + 1;
+        }
+        if (!dead && !wait_for(bar, parity)) dead = true;
+        parity ^= 1;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        load_sums();
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        take();
+        const unsigned o = tile * TILE + row;
+        const bool two = cols >> 31;                             // (fp32: pairs of columns are one row of x)
+        const unsigned n_cols = cols & 0x7fffffffu;
+        if (o < w.d_out) {
+#pragma unroll
+            for (int c = 0; c < N; c += 2) {
+                const unsigned col = blockIdx.y * N + c;
+                if (col >= n_cols) break;
+                const float u = total[c] * p.undo[col], v = col + 1 < n_cols ? total[c + 1] * p.undo[col + 1] : 0.f;
+                if (two) {
+                    store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, (u + v) * 0x1p24f);
+                } else {
+                    store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, u * 0x1p24f);
+                    if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, v * 0x1p24f);
+                }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (dead) atomicOr(status, ST_TIMEOUT);
+    __syncthreads();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(M::TMEM));
+}
+
+template <int G, bool OFFSETS, int N>
+int wide_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, unsigned rows, const bf_rows& y, Prepared p) {
+    using M = Wide<G, OFFSETS, N>;
+    const bool two = x.type == BF_F32;
+    const unsigned cols = rows * (two ? 2 : 1), chunks = (cols + N - 1) / N, tiles = (w.d_out + TILE - 1) / TILE;
+    q4_prepare_kernel<G><<<rows, PREP_WARPS * 32, 0, t->stream>>>(x, row0, w.d_in, rows_wide(&x, false), p);
+    if (int rc = launched(t, "q4_prepare_kernel")) return rc;
+    const unsigned stages = 2, bytes = stages * M::STAGE + (stages + 1) * M::SUMS + 1024;
+    unsigned per_sm = SMEM_MAX / (bytes + 1024 + 256);
+    if (per_sm > 512 / M::TMEM) per_sm = 512 / M::TMEM;          // (a block that finds no TMEM would wait for one that ends)
+    cudaError_t e = room_for<q4_wide_kernel<G, OFFSETS, N>>(t, SMEM_MAX - 1024);
+    if (e != cudaSuccess) return cuda_failed(t, "cudaFuncSetAttribute", e);
+    cudaLaunchConfig_t cfg = {};
+    const unsigned most = t->n_sm * per_sm / (chunks < per_sm ? chunks : per_sm);
+    cfg.gridDim = dim3(tiles < most ? tiles : most, chunks);
+    cfg.blockDim = TILE;
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = t->stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, q4_wide_kernel<G, OFFSETS, N>, w, p, cols | (two ? 1u << 31 : 0), stages, y, row0, t->status);
+    return e == cudaSuccess ? launched(t, "q4_wide_kernel") : cuda_failed(t, "q4_wide_kernel", e);
+}
+
+// Rows of W from which blocks of 128 of them are faster than blocks that share the columns out as well.  4096 columns, groups of 128,
+// us with the former and the latter: 128256 rows, 16 / 32 / 64 rows of x 80 and 88 / 105 and 144 / 157 and 220; 4096 rows 29 and 11 /
+// 33 and 24 / 36 and 63.  (Groups of 32 with 64 columns would need more registers for sums than there are.)
+template <int G> bool wide_pays(const bf_trusted* t, unsigned d_out, unsigned width) {
+    if (width < 16 || TILE / G * width > 128) return false;
+    return (d_out + TILE - 1) / TILE >= (unsigned)t->n_sm / (width == 64 ? 8 : 1);
+}
 template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned n, const bf_rows& y) {
     const unsigned per_row = x.type == BF_F32 ? 2 : 1, segs = (w.d_in + SEG - 1) / SEG;
     // every block of the first kernel makes the operands of x itself
@@ -633,12 +904,21 @@ template <int G, bool OFFSETS> int linear(bf_trusted* t, const Q4& w, const bf_r
         if (chunks || p.width == 8) break;
     }
     if (chunks == 0) return BF_ERR_TOO_LARGE;
+    p.tiled = wide_pays<G>(t, w.d_out, p.width);
     if (chunks > 1024) chunks = 1024;
     const unsigned rows_at_once = (unsigned)(chunks * p.width / per_row);
     for (unsigned r = 0; r < n; r += rows_at_once) {
         const unsigned rows = n - r < rows_at_once ? n - r : rows_at_once;
         p.undo = reinterpret_cast<float*>(t->ws);
         p.at = t->ws + (((size_t)rows * per_row + p.width) * 4 + 255) / 256 * 256;
+        if (p.tiled) {
+            int rc;
+            if (p.width == 16) rc = wide_launch<G, OFFSETS, 16>(t, w, x, r, rows, y, p);
+            else if (p.width == 32) rc = wide_launch<G, OFFSETS, 32>(t, w, x, r, rows, y, p);
+            else rc = wide_launch<G, OFFSETS, G == 32 ? 32 : 64>(t, w, x, r, rows, y, p);       // (groups of 32 do not come here)
+            if (rc) return rc;
+            continue;
+        }
         int rc = p.width == 8    ? many_launch<G, OFFSETS, 1>(t, w, x, r, rows, y, p)
                  : p.width == 16 ? many_launch<G, OFFSETS, 2>(t, w, x, r, rows, y, p)
                  : p.width == 32 ? many_launch<G, OFFSETS, 4>(t, w, x, r, rows, y, p)

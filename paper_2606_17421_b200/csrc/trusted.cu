@@ -60,7 +60,7 @@ extern "C" int bf_trusted_status(bf_trusted* t) {
     if (e == cudaSuccess) e = cudaMemsetAsync(t->status, 0, sizeof(int), t->stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(t->stream);
     if (e != cudaSuccess) return cuda_failed(t, "bf_trusted_status", e);
-    return found & ST_RANGE ? BF_ERR_RANGE : found & ST_OOM ? BF_ERR_OOM : BF_OK;
+    return found & ST_TIMEOUT ? BF_ERR_TIMEOUT : found & ST_RANGE ? BF_ERR_RANGE : found & ST_OOM ? BF_ERR_OOM : BF_OK;
 }
 
 extern "C" uint64_t bf_kv4_block_bytes(uint32_t head_dim, uint32_t group, uint32_t page_tokens) {

@@ -219,7 +219,10 @@ def linear_tolerance(x, y, top, ytype):
 
 LINEAR = [(1, 64, 16, 32), (1, 64, 17, 64), (1, 1, 1, 32), (1, 33, 5, 128), (2, 200, 129, 64), (3, 768, 300, 128), (7, 1000, 77, 32), (8, 1024, 64, 128), (9, 96, 2500, 32),
           (16, 2048, 130, 64), (17, 511, 33, 128), (31, 640, 50, 32), (33, 1500, 100, 64), (64, 256, 1000, 128), (65, 320, 47, 64), (130, 160, 40, 32), (1, 14336, 40, 128),
-          (5, 9000, 20, 64), (40, 5000, 24, 128)]
+          (5, 9000, 20, 64), (40, 5000, 24, 128),
+          # rows enough for blocks of 128: odd last tiles, one stage and several, columns behind the last
+          (9, 256, 18944, 128), (16, 300, 19001, 64), (13, 600, 19072, 32), (32, 1100, 18945, 128), (25, 64, 20000, 32), (20, 513, 19000, 64), (64, 700, 2500, 128),
+          (41, 1500, 2305, 64), (100, 257, 2400, 128), (60, 320, 19000, 32)]
 
 
 @gpu
