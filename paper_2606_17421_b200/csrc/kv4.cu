@@ -260,9 +260,10 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 //   O^T = V^T (p scale): channels x rows, codes taken the same way; p^T by a transposition in registers, times the scale of each
 //         token and group relative to a power of two that follows the largest.  The lows are a product of their own, a row a group.
 // Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
-// Bound by HBM for single tokens: 2.2 instructions a code at D = 128 against the 2.8 that the copy rate leaves time for.
+// Single tokens are bound by issue: about 280 instructions a sub-block of 2.2 KB at D = 128, half of them unpacking and scores, in 55 % of
+// the slots (131072 tokens, 32 query heads: 39 us, 3.6 TB/s); few tokens by the chain of length, table, first copy and joining.
 constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
-constexpr float P_SLACK = 8.f, NO_BASE = 1e30f;
+constexpr float P_SLACK = 8.f, NO_BASE = __builtin_huge_valf();
 constexpr unsigned PIECE = 128, MOST_SPLITS = 160;          // (what 8 NT rows of them count for fits where the copies were)
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -313,15 +314,13 @@ struct Att {
     int wide;
 };
 
-// Row r of a block's rows: its token's number in the sequence's rows, its query head
-struct Row {
-    int j, head;
-};
+// The first token that a row at `pos` sees.  (A window may be as large as it likes, and a position below zero.)
+__device__ __forceinline__ int first_seen(int pos, unsigned window) { return window ? (int)max(0ll, (long long)pos + 1 - window) : 0; }
 
 // Parameters of values where some row does not see some token.  What no row sees may be anything; a NaN that some rows see and others
 // do not is taken out of the product, and given to the channels of those that do.
 template <int D, int G, int NT>
-__device__ __forceinline__ void give_nan(unsigned odd, int e, float (&o)[D / 16][NT][4], int t0, const int (&pos)[NT][2], int win) {
+__device__ __forceinline__ void give_nan(unsigned odd, int e, float (&o)[D / 16][NT][4], int t0, const int (&pos)[NT][2], unsigned window) {
 #pragma unroll 1
     for (int u = 0; u < 16; ++u) {
         const unsigned theirs = __shfl_sync(~0u, odd, u / 2 % 4);
@@ -330,14 +329,14 @@ __device__ __forceinline__ void give_nan(unsigned odd, int e, float (&o)[D / 16]
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                if (t0 + u <= pos[n][h] && t0 + u > pos[n][h] - win)
+                if (t0 + u <= pos[n][h] && t0 + u >= first_seen(pos[n][h], window))
 #pragma unroll
                     for (int t = 0; t < D / 16; ++t)
                         if (t * 16 / G == e) o[t][n][h] = o[t][n][h + 2] = CUDART_NAN_F;
     }
 }
 template <int D, int G, int NT>
-__device__ __forceinline__ void open_values(uint4 (&par)[D / G], float (&o)[D / 16][NT][4], int t0, int from, int to, const int (&pos)[NT][2], int win, int j4) {
+__device__ __forceinline__ void open_values(uint4 (&par)[D / G], float (&o)[D / 16][NT][4], int t0, int from, int to, const int (&pos)[NT][2], unsigned window, int j4) {
 #pragma unroll
     for (int e = 0; e < D / G; ++e) {
         uint32_t w[4] = {par[e].x, par[e].y, par[e].z, par[e].w};
@@ -354,7 +353,7 @@ __device__ __forceinline__ void open_values(uint4 (&par)[D / G], float (&o)[D / 
             if (seen && off) odd |= 1u << k;
         }
         par[e] = make_uint4(w[0], w[1], w[2], w[3]);
-        if (__any_sync(~0u, odd)) give_nan<D, G, NT>(odd, e, o, t0, pos, win);
+        if (__any_sync(~0u, odd)) give_nan<D, G, NT>(odd, e, o, t0, pos, window);
     }
 }
 
@@ -384,8 +383,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     // tokens that some row of this block sees, those that every row sees, and this block's share of the sub-blocks
     const int before = s.len - s.rows;                                       // position of the sequence's first row
     const int pos_first = before + (int)p.per.quotient(r0), pos_last = before + (int)p.per.quotient(min(r0 + RW, rows) - 1);
-    const int win = p.window ? (int)min(p.window, 0x7fffffffu) : 0x7fffffff;
-    const int from = max(0, pos_first - win + 1), to = pos_last + 1, all_from = max(0, pos_last - win + 1), all_to = pos_first + 1;
+    const int from = first_seen(pos_first, p.window), to = pos_last + 1, all_from = first_seen(pos_last, p.window), all_to = pos_first + 1;
     const int sb0 = from / 16, n_sb = to > from ? (to + 15) / 16 - sb0 : 0, each = max(p.each, (int)p.splits.quotient(n_sb + p.splits.d - 1));
     const unsigned n_splits = max(1, (n_sb + each - 1) / each);              // of this row's tokens
     if (split >= n_splits) return;
@@ -592,7 +590,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         uint4 par[E];                                                        // of the values, for later
 #pragma unroll
         for (int e = 0; e < E; ++e) par[e] = reinterpret_cast<const uint4*>(sub + S::V_PAR)[e * 4 + j4];
-        if (masked) open_values<D, G, NT>(par, o, t0, from, to, pos, win, (int)j4);
+        if (masked) open_values<D, G, NT>(par, o, t0, from, to, pos, p.window, (int)j4);
         bool over = false;
         float y[NT][4];
 #pragma unroll
@@ -602,7 +600,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                 y[n][k] = fmaf(x[n][k], coef[n][k % 2], base[n][k % 2]);
                 if (masked) {
                     const int t = t0 + (int)g + k / 2 * 8;
-                    if (t > pos[n][k % 2] || t <= pos[n][k % 2] - win) y[n][k] = -CUDART_INF_F;
+                    if (t > pos[n][k % 2] || t < first_seen(pos[n][k % 2], p.window)) y[n][k] = -CUDART_INF_F;
                 }
             }
             over |= fmaxf(y[n][0], y[n][2]) > P_UP + P_SLACK;

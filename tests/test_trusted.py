@@ -513,6 +513,18 @@ def test_attention_pages_lists_and_hints(side, T):
 
 
 @gpu
+def test_attention_more_rows_than_tokens_and_large_windows(side):
+    """Rows far before the first token see nothing, those behind it all there is, whatever the window's size."""
+    torch = side.torch
+    c = ref.Cache(1, 12, 2, 64, 32, 16, 3, 4)
+    d = fill(side, c, [20, 1, 0])
+    q = torch.randn((90, 4, 64), device="cuda").half()
+    for window in (0, 1, 7, 2 ** 31 - 1, 2 ** 31, 2 ** 32 - 1):
+        check_attention(side, d, 0, None, [45, 30, 15], q, 4, window, "fp16", max_len=20)
+    assert status_of(side) == 0
+
+
+@gpu
 def test_attention_extreme_scores(side):
     """Scores far apart, all alike, far below zero, and a growing row of them; a NaN in q stays in its row."""
     torch = side.torch
