@@ -123,7 +123,11 @@ __device__ __forceinline__ void x_unit(float (&v)[8], float big, bool two, Place
 
 // Up to 8 columns of x that fit shared memory whole.  A warp takes 16 rows of W and every KW-th stage of 256 columns, brings the codes in by
 // asynchronous copies, STAGES - 1 ahead and without a barrier of the block, and multiplies them from there.
+// 4096 x 128256, one row: 54 us (5.0 TB/s of the 6.5 that a copy reaches); half of the issue slots, 250 instructions a stage of 2.1 KB, are
+// what is next.  With the eight 16-byte pieces of a row's stage in eight lines of shared memory instead of one it took 87, with 32
+// warps a block of 64 registers 61.  Small matrices are a launch, x and one or two stages.
 constexpr unsigned STAGES = 4, X_AT_ONCE = 4, MOST_WARPS = 16;
+static_assert((MOST_WARPS & (MOST_WARPS - 1)) == 0, "warps along the columns, a power of two, have to divide a block's");
 template <int G, bool OFFSETS> struct Stage { static constexpr unsigned BYTES = CODE_BYTES + 16 * (SEG / G) * 2 * (OFFSETS ? 2 : 1); };
 
 // the parameters that a row has in a stage: 2, 4 or 8 fp16 numbers
@@ -396,7 +400,8 @@ __global__ void __launch_bounds__(PREP_WARPS * 32) q4_prepare_kernel(bf_rows x, 
 }
 
 // A block of 8 warps, kw of them along the columns; a warp has 32 rows of W, 8 NT columns.  All warps go through the stages together: a
-// stage holds kw times 256 columns of the rows and of x.
+// stage holds kw times 256 columns of the rows and of x.  14336 x 4096, 8 rows: 18 us with the kernel before it, 7 steps of 2 us: the
+// latency of a step with its barrier.  32 rows of x and 128256 of W: 144 us, the matrix instructions busy in half of them.
 constexpr unsigned MANY_WARPS = 8, ROWS = 32;
 template <int G, bool OFFSETS> struct Many {
     static constexpr unsigned GROUPS = SEG / G, PAR = GROUPS * 2, CODES = ROWS * SEG / 2, WARP = CODES + ROWS * PAR * (OFFSETS ? 2 : 1);
@@ -626,6 +631,8 @@ constexpr unsigned FEW_UNITS = 32;
 // the order in which a word unpacks); x is operand B in shared memory, rows of 128 bytes in the 128-byte swizzle; one thread issues
 // the products of a group of columns into its own accumulators, and each thread multiplies its row's sums by the group's scale.
 // While the products run, the next 128 columns are unpacked.  Waits are bounded; one that gives up is BF_ERR_TIMEOUT.
+// 4096 x 128256, 32 rows: 104 us (2.7 TB/s); three blocks an SM, which shared memory allows, keep 46 % of the issue slots busy, and 1002
+// tiles are 2.3 rounds of them.  With two blocks (210 registers a thread) 138.
 constexpr unsigned TILE = 128;
 
 __device__ __forceinline__ bool wait_for(uint32_t bar, unsigned parity) {
