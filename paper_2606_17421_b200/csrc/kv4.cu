@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 //   O^T = V^T (p scale): channels x rows, codes taken the same way; p^T by a transposition in registers, times the scale of each
 //         token and group relative to a power of two that follows the largest.  The lows are a product of their own, a row a group.
 // Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
-// Single tokens are bound by issue: about 280 instructions a sub-block of 2.2 KB at D = 128, half of them unpacking and scores, in 55 % of
-// the slots (131072 tokens, 32 query heads: 39 us, 3.6 TB/s); few tokens by the chain of length, table, first copy and joining.
+// Single tokens are bound by issue: about 300 instructions a sub-block of 2.2 KB at D = 128, half of them unpacking and scores, in 55 % of
+// the slots (131072 tokens, 32 query heads: 40 us, 3.5 TB/s); few tokens by the chain of length, table, first copy and joining.
 constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
 constexpr float P_SLACK = 8.f, NO_BASE = __builtin_huge_valf();
 constexpr unsigned PIECE = 128, MOST_SPLITS = 160;          // (what 8 NT rows of them count for fits where the copies were)
