@@ -1,7 +1,8 @@
 /*
  * libbifrost: the accelerator-side CKKS linear layer of a hybrid TEE-FHE serving stack, for one
  * NVIDIA B200 (sm_100a).  The trusted side (key generation, encryption, decryption, non-linear
- * operators) is not here: callers hand in ciphertexts and rotation keys as plain arrays.
+ * operators) is not here: callers hand in ciphertexts and rotation keys as plain arrays.  Of its work on plaintext, attention over a KV
+ * cache, the cache's pages and 4-bit projections are: see bf_trusted.
  *
  * Conventions shared by all entry points
  *   - Every function returns BF_OK (0) or a negative BF_ERR_* code; nothing throws or aborts.
