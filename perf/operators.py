@@ -264,16 +264,17 @@ def prepare(case, seed):
 
 # ---------------------------------------------------------------------------------------------- the framework's calls
 
-_trusted = None
+_trusted = {}
 
 
 def _context():
-    """The one context that a program's trusted half has."""
-    global _trusted
-    if _trusted is None:
-        from paper_2606_17421_b200 import bifrost as bf
-        _trusted = bf, bf.bf_trusted_create(0, torch.cuda.current_stream().cuda_stream)
-    return _trusted
+    """The context that a program's trusted half has on the stream that its inputs were made on: one for each device and stream."""
+    from paper_2606_17421_b200 import bifrost as bf
+    stream = torch.cuda.current_stream()
+    key = stream.device_index, stream.cuda_stream
+    if key not in _trusted:
+        _trusted[key] = bf.bf_trusted_create(0, stream.cuda_stream)
+    return bf, _trusted[key]
 
 
 def _cache(bf, s):
