@@ -256,7 +256,7 @@ def prepare(case, seed):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
     s = _State()
-    s.case = case
+    s.case, s.device = case, torch.cuda.current_device()
     (_prepare_linear if case["op"] == "linear" else _prepare_cache)(s, case, gen)
     torch.cuda.synchronize()
     return s
@@ -267,14 +267,15 @@ def prepare(case, seed):
 _trusted = {}
 
 
-def _context():
-    """The context that a program's trusted half has on the stream that its inputs were made on: one for each device and stream."""
-    from paper_2606_17421_b200 import bifrost as bf
-    stream = torch.cuda.current_stream()
-    key = stream.device_index, stream.cuda_stream
-    if key not in _trusted:
-        _trusted[key] = bf.bf_trusted_create(0, stream.cuda_stream)
-    return bf, _trusted[key]
+def _context(s):
+    """The context that a program's trusted half has on the stream in which its inputs are used: one for each device and stream."""
+    key = s.device, torch._C._cuda_getCurrentRawStream(s.device)
+    held = _trusted.get(key)
+    if held is None:
+        from paper_2606_17421_b200 import bifrost as bf
+        with torch.cuda.device(s.device):
+            held = _trusted[key] = bf, bf.bf_trusted_create(0, key[1])
+    return held
 
 
 def _cache(bf, s):
@@ -283,14 +284,14 @@ def _cache(bf, s):
 
 
 def _own_linear(s):
-    bf, t = _context()
+    bf, t = _context(s)
     W = bf.bf_q4_matrix.of(s.codes, s.scales, s.offsets, s.case["d_in"], s.case["group"])
     bf.bf_q4_linear(t, W, bf.bf_rows.of(s.x), s.case["n"], bf.bf_rows.of(s.y))
     return {"y": s.y}
 
 
 def _own_attend(s):
-    bf, t = _context()
+    bf, t = _context(s)
     c = s.case
     starts = s.starts if c["tokens"] > 1 else None          # one token a sequence needs no list of starts
     bf.bf_kv4_attention(t, _cache(bf, s), s.layer, None, starts, c["seqs"], c["tokens"], c["longest"], bf.bf_rows.of(s.q), c["heads"],
@@ -299,7 +300,7 @@ def _own_attend(s):
 
 
 def _own_store(s):
-    bf, t = _context()
+    bf, t = _context(s)
     c = s.case
     cache = _cache(bf, s)
     starts = s.starts if c["tokens"] > 1 else None
@@ -309,7 +310,7 @@ def _own_store(s):
 
 
 def _own_fork(s):
-    bf, t = _context()
+    bf, t = _context(s)
     cache = _cache(bf, s)
     bf.bf_kv4_free(t, cache, s.children, s.case["seqs"])
     bf.bf_kv4_fork(t, cache, s.parents, s.children, s.case["seqs"])
@@ -317,7 +318,7 @@ def _own_fork(s):
 
 
 def _own_compact(s):
-    bf, t = _context()
+    bf, t = _context(s)
     bf.bf_kv4_compact(t, _cache(bf, s), s.new_tables, s.new_refs, s.n_live)
     return {"tables": s.new_tables, "refs": s.new_refs, "n_live": s.n_live, "pool": s.pool}
 
