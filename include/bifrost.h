@@ -420,8 +420,9 @@ int bf_kv4_read(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int3
  *     out = sum_t softmax_t(scale * <q, K_t>) V_t
  * Cache values behind a sequence's length are never used, whatever they are.  A row that sees nothing (an empty sequence, more rows
  * than tokens) becomes zeros.  lse (device, fp32 [rows][n_q_heads], or NULL) receives log sum exp, -inf for such a row: results
- * over several caches are joined with it.  Products with the codes are exact, scores, softmax and sums in 32 bits; probabilities
- * and values enter the second product in fp16 (half a step, 2^-11, of each).
+ * over several caches are joined with it.  Products with the codes are exact, scores, softmax and sums in 32 bits. In the second
+ * product a probability is held in fp16 (half a step, 2^-11 of it, or 2^-31 of the row's largest where that is more), and so is the value, or, with 8
+ * rows of a key head or fewer, the probability times the value's scale (2^-11 of |low| + 15 scale): whatever the other tokens' scales are.
  * max_q: most rows of a sequence (one with more is RANGE, its rows are left alone); max_len: a length that the work is
  * divided for (any is right).  out: the type of q, any strides; it may not overlap q.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
 int bf_kv4_attention(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int32_t* seqs, const int32_t* starts, uint32_t n,

@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 //   softmax over tokens with a maximum per row that is only moved when a score exceeds it by 2^8: a vote a sub-block in the
 //         place of three exchanges.  p is held 2^6 up, so that fp16 takes what lies down to 2^-30 of the largest.
 //   O^T = V^T (p scale): channels x rows, codes taken the same way; p^T by a transposition in registers, times the scale of each
-//         token and group relative to a power of two that follows the largest.  The lows are a product of their own, a row a group.
+//         token and group relative to a power of two that follows them (follow_scales).  The lows are a product of their own, a row a group.
 // Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
 // Single tokens are bound by issue: about 300 instructions a sub-block of 2.2 KB at D = 128, half of them unpacking and scores, in 55 % of
 // the slots (131072 tokens, 32 query heads: 40 us, 3.5 TB/s); few tokens by the chain of length, table, first copy and joining.
@@ -355,6 +355,46 @@ __device__ __forceinline__ void open_values(uint4 (&par)[D / G], float (&o)[D / 
         par[e] = make_uint4(w[0], w[1], w[2], w[3]);
         if (__any_sync(~0u, odd)) give_nan<D, G, NT>(odd, e, o, t0, pos, window);
     }
+}
+
+// Scales of the values of 16 tokens in one group as the products take them: two a register (every lane with the same j4 has the same),
+// relative to a power of two, 2^-14 .. 2^15, of which `inv` is the inverse.  It is 1 at first, which suits scales from 2^-7 to 2, and 2 to 4 times
+// the largest when it is set; and it is set when one exceeds it twice (with p < 2^14 fp16 holds that) or one falls below 2^-7 of
+// it: fp16 would lose bits of a smaller one, alone (below 2^-14) or with a probability.  What is small beside others is left out, as 0,
+// for products of its own.  Returns whether there is any; `f` is what earlier sums are to be multiplied by.
+constexpr float LEAST_RATIO = 0x1p-7f, MOST_RATIO = 2.f, LEAST_REF = 0x1p-14f;   // (relative to the least nothing is below 2^-10)
+__device__ __forceinline__ float below_of(__half2 inv) {
+    const float i = __low2float(inv);
+    return i < 1.f / LEAST_REF ? LEAST_RATIO / i : 0.f;
+}
+__device__ __forceinline__ bool follow_scales(uint32_t (&s)[2], __half2& inv, float& f) {
+    float v[4], top = 0, least = CUDART_INF_F;                               // of what is not 0; both pass over a NaN
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2 h = half2_of(s[k / 2]);
+        v[k] = fabsf(k % 2 ? __high2float(h) : __low2float(h));
+        top = fmaxf(top, v[k]);
+        if (v[k] > 0) least = fminf(least, v[k]);
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        least = fminf(least, __shfl_xor_sync(~0u, least, d));
+    }
+    const float old = 1.f / __low2float(inv);
+    f = 1.f;
+    if (top > MOST_RATIO * old || least < below_of(inv)) {
+        const float now = fminf(fmaxf(__uint_as_float((__float_as_uint(fminf(top, 32768.f)) & 0x7f800000u) + 0x01000000u), LEAST_REF), 32768.f);
+        f = old / now;
+        inv = __float2half2_rn(1.f / now);
+    }
+    const float below = below_of(inv);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (v[k] < below) s[k / 2] &= ~(0xffffu << (16 * (k % 2)));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) s[k] = bits(__hmul2(half2_of(s[k]), inv));
+    return least < below;
 }
 
 template <int D, int G, int NT>
@@ -504,9 +544,10 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     float held_sum[HOLD ? E : 1][HOLD ? NT : 1][2];
     float coef[NT][2], base[NT][2], l[NT][2] = {}, o[MT][NT][4] = {};   // base: P_UP - the maximum that is held
     float low[NT][4] = {};                                                   // of group g's lows
-    __half2 ref[E], inv_ref[E];
+    __half2 inv_ref[E];                                                      // see follow_scales
 #pragma unroll
-    for (int e = 0; e < E; ++e) ref[e] = __float2half2_rn(0.f), inv_ref[e] = __float2half2_rn(0.f);
+    for (int e = 0; e < E; ++e) inv_ref[e] = __float2half2_rn(1.f);
+    __half2 my_inv = inv_ref[0];                                             // of group g % E
     int pos[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -591,7 +632,46 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
         for (int e = 0; e < E; ++e) par[e] = reinterpret_cast<const uint4*>(sub + S::V_PAR)[e * 4 + j4];
         if (masked) open_values<D, G, NT>(par, o, t0, from, to, pos, p.window, (int)j4);
-        bool over = false;
+        bool apart = false;                                                  // scales too far from what they are held relative to
+        if (SCALE_P) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) par[e].x = bits(__hmul2(half2_of(par[e].x), inv_ref[e])), par[e].y = bits(__hmul2(half2_of(par[e].y), inv_ref[e]));
+            // each group is looked at by the lanes whose g is its number, not by all.  (Behind a border that may be anything: a look too many)
+            __half2 s01 = half2_of(par[0].x), s89 = half2_of(par[0].y);
+            if (E > 1) {
+                const uint2 w = *reinterpret_cast<const uint2*>(sub + S::V_PAR + (g % E * 4 + j4) * 16);
+                s01 = __hmul2(half2_of(w.x), my_inv), s89 = __hmul2(half2_of(w.y), my_inv);
+            }
+            apart = __any_sync(~0u, !__hbge2(__hmin2(s01, s89), __float2half2_rn(LEAST_RATIO)) || !__hble2(__hmax2(s01, s89), __float2half2_rn(MOST_RATIO)));
+        }
+        bool over = false, left = false;                                     // left: scales of values that the products leave out for now
+        auto take_scales = [&](bool again) {                                 // of all tokens, or of those that were left out
+            left = false;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const uint2 w = *reinterpret_cast<const uint2*>(sub + S::V_PAR + (e * 4 + j4) * 16);
+                uint32_t s[2] = {w.x, w.y};
+                const float below = again ? below_of(inv_ref[e]) : CUDART_INF_F;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned sh = 16 * (k % 2), a = s[k / 2] >> sh & 0x7fff;
+                    const int t = t0 + 2 * (int)j4 + k % 2 + k / 2 * 8;
+                    const bool in = (!masked || (t >= from && t < to && a < 0x7c00)) && (!again || __half2float(__ushort_as_half((unsigned short)a)) < below);
+                    if (!in) s[k / 2] &= ~(0xffffu << sh);
+                }
+                float f;
+                left |= follow_scales(s, inv_ref[e], f);
+                par[e].x = s[0], par[e].y = s[1];
+                if ((int)g % E == e) my_inv = inv_ref[e];
+                if (f != 1.f)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[t][n][k] *= f;
+            }
+        };
         float y[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -605,10 +685,6 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
             }
             over |= fmaxf(y[n][0], y[n][2]) > P_UP + P_SLACK;
             over |= fmaxf(y[n][1], y[n][3]) > P_UP + P_SLACK;
-        }
-        if (SCALE_P) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) over |= !__hbge2(ref[e], __hmax2(__habs2(half2_of(par[e].x)), __habs2(half2_of(par[e].y))));
         }
         if (__any_sync(~0u, over)) {
 #pragma unroll
@@ -631,30 +707,6 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                         y[n][h + 2] = v + base[n][h];
                     }
                 }
-            if (SCALE_P) {
-                // scales are taken relative to a power of two that is at least the largest so far
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const __half2 h = __hmax2(__habs2(half2_of(par[e].x)), __habs2(half2_of(par[e].y)));
-                    float top = fmaxf(__low2float(h), __high2float(h));      // (passes over a NaN)
-#pragma unroll
-                    for (int d = 1; d < 4; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-                    const float old = __low2float(ref[e]);
-                    if (top > old) {
-                        // 2^15 at most, 2^-14 at least: ref and its inverse are both fp16 numbers
-                        const float now = top >= 32768.f ? 32768.f : fmaxf(__uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u), 0x1p-14f);
-                        const float f = old / now;
-                        ref[e] = __float2half2_rn(now);
-                        inv_ref[e] = __float2half2_rn(1.f / now);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int t = e * (G / 16); t < (e + 1) * (G / 16); ++t)
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) o[t][n][k] *= f;
-                    }
-                }
-            }
         }
         uint32_t pb[NT][2];
 #pragma unroll
@@ -668,17 +720,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         }
 
         // values of tokens 2 j4, 2 j4 + 1 and those 8 behind, channels g and g + 8 of 16
-        uint32_t ps[SCALE_P ? E : 1][NT][2];
         if (SCALE_P) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const __half2 s01 = __hmul2(half2_of(par[e].x), inv_ref[e]), s89 = __hmul2(half2_of(par[e].y), inv_ref[e]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    ps[SCALE_P ? e : 0][n][0] = bits(__hmul2(half2_of(pb[n][0]), s01));
-                    ps[SCALE_P ? e : 0][n][1] = bits(__hmul2(half2_of(pb[n][1]), s89));
-                }
-            }
             uint32_t m01 = 0, m89 = 0;
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -686,27 +728,54 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma(low[n], m01, 0u, m89, 0u, pb[n][0], pb[n][1]);
         }
+        auto add_values = [&]() {
+            uint32_t ps[SCALE_P ? E : 1][NT][2];
+            if (SCALE_P) {
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-            const uint4 w4 = reinterpret_cast<const uint4*>(sub + S::V_CODE)[c * 32 + lane];
-            const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+                for (int e = 0; e < E; ++e) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = 4 * c + k, e = t * 16 / G;
-                const uint32_t w = word[k], v = w >> 8;
-                if (SCALE_P) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma(o[t][n], w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u, ps[SCALE_P ? e : 0][n][0], ps[SCALE_P ? e : 0][n][1]);
-                } else {
-                    const __half2 k1024 = __floats2half2_rn(1024.f, 1024.f), k16 = __floats2half2_rn(0.0625f, 0.0625f), k64 = __floats2half2_rn(-64.f, -64.f);
-                    const __half2 s01 = half2_of(par[e].x), s89 = half2_of(par[e].y), m01 = half2_of(par[e].z), m89 = half2_of(par[e].w);
-                    const __half2 c0 = __hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), k1024), c1 = __hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), k16, k64);
-                    const __half2 c2 = __hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), k1024), c3 = __hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), k16, k64);
-                    const uint32_t a0 = bits(__hfma2(c0, s01, m01)), a1 = bits(__hfma2(c1, s01, m01)), a2 = bits(__hfma2(c2, s89, m89)), a3 = bits(__hfma2(c3, s89, m89));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) mma(o[t][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                    for (int n = 0; n < NT; ++n) {
+                        ps[SCALE_P ? e : 0][n][0] = bits(__hmul2(half2_of(pb[n][0]), half2_of(par[e].x)));
+                        ps[SCALE_P ? e : 0][n][1] = bits(__hmul2(half2_of(pb[n][1]), half2_of(par[e].y)));
+                    }
                 }
+            }
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                const uint4 w4 = reinterpret_cast<const uint4*>(sub + S::V_CODE)[c * 32 + lane];
+                const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int t = 4 * c + k, e = t * 16 / G;
+                    const uint32_t w = word[k], v = w >> 8;
+                    if (SCALE_P) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma(o[t][n], w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u, ps[SCALE_P ? e : 0][n][0], ps[SCALE_P ? e : 0][n][1]);
+                    } else {
+                        const __half2 k1024 = __floats2half2_rn(1024.f, 1024.f), k16 = __floats2half2_rn(0.0625f, 0.0625f), k64 = __floats2half2_rn(-64.f, -64.f);
+                        const __half2 s01 = half2_of(par[e].x), s89 = half2_of(par[e].y), m01 = half2_of(par[e].z), m89 = half2_of(par[e].w);
+                        const __half2 c0 = __hsub2(half2_of((w & 0x000f000fu) | 0x64006400u), k1024), c1 = __hfma2(half2_of((w & 0x00f000f0u) | 0x64006400u), k16, k64);
+                        const __half2 c2 = __hsub2(half2_of((v & 0x000f000fu) | 0x64006400u), k1024), c3 = __hfma2(half2_of((v & 0x00f000f0u) | 0x64006400u), k16, k64);
+                        const uint32_t a0 = bits(__hfma2(c0, s01, m01)), a1 = bits(__hfma2(c1, s01, m01)), a2 = bits(__hfma2(c2, s89, m89)), a3 = bits(__hfma2(c3, s89, m89));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma(o[t][n], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+                    }
+                }
+            }
+        };
+        if (!SCALE_P || !apart) {
+            add_values();
+        } else {
+            uint2* stash = reinterpret_cast<uint2*>(my_ring + (sub - my_ring)) + lane;   // where the codes of keys were: no registers for what is rare
+            __syncwarp();
+            *stash = make_uint2(pb[0][0], pb[0][1]);
+            for (bool again = false;; again = true) {
+                take_scales(again);
+                add_values();
+                if (!left) break;
+                const uint2 kept = *stash;
+                pb[0][0] = kept.x, pb[0][1] = kept.y;
             }
         }
         __syncwarp();                                                        // the slot is free for the next copy
@@ -717,7 +786,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     // codes were taken as 2^-24 (channels g) and 2^-20 (g + 8) of themselves, scales relative to ref
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float f = __low2float(ref[e]);
+        const float f = 1.f / __low2float(inv_ref[e]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll

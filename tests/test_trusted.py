@@ -1035,3 +1035,27 @@ def test_layers_beyond_32_bits_of_offset(side):
     for x, held in ((k, kk), (v, vv)):
         span = (x.float().amax(-1, keepdim=True) - x.float().amin(-1, keepdim=True))
         assert bool(((x.float() - held.float()).abs() <= span / 30 + 2.0 ** -10 * (span + x.float().abs().amax(-1, keepdim=True)) + 2.0 ** -11 * held.float().abs()).all())
+
+
+@gpu
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_attention_beside_values_that_do_not_count(side, D, G):
+    """Tokens with huge values and next to no weight leave the bits of the others' values alone: single tokens and chunks, huge ones first, last
+    and in between, several orders of magnitude in one sub-block."""
+    torch = side.torch
+    for seed, sizes in enumerate(([30000.0, 0.5], [30000.0, 0.03], [60000.0, 1e-3], [50000.0, 40.0, 0.05], [2000.0, 1.0])):
+        rng = np.random.default_rng([D, G, seed])
+        c = ref.Cache(1, 24, 1, D, G, 16, 1, 20)
+        c.grow([0], [300])
+        hidden = {0: 0, 3: -1, 5: 0, 17: -2, 150: 0, 155: 1, 156: -2, 299: 0}               # which token has which size; the rest have the last
+        for t in range(300):
+            size = sizes[hidden.get(t, -1)]
+            k, v = rng.standard_normal((1, D)), rng.uniform(-1, 1, (1, D)) * size
+            k[0, 0] = 0.0 if size == sizes[-1] else -100.0
+            c.put(0, 0, t, k, v)
+        d = DeviceCache(side, c)
+        q = torch.from_numpy(rng.standard_normal((12, 4, D))).cuda().half()
+        q[:, :, 0] = 12.0                                                                   # exp(-100) and less for what is hidden
+        for counts, heads in (([1], 4), ([1], 1), ([2], 4), ([4], 4), ([12], 4)):
+            check_attention(side, d, 0, [0], counts, q[:counts[0], :heads], heads, 0, "fp16")
+    assert status_of(side) == 0
