@@ -46,7 +46,9 @@ class TrustedHalf:
             self.lengths = torch.zeros(seqs, dtype=torch.int32, device=self.device)
             self.refs = torch.zeros(n_pages, dtype=torch.int32, device=self.device)
             self.cache = bf.bf_kv4_cache.of(self.pool, self.tables, self.lengths, self.refs, m.head_dim, group, page_tokens)
+            # lists that kernels read in later steps are made once, on the stream that reads them
             self.all_seqs = torch.arange(seqs, dtype=torch.int32, device=self.device)
+            self.prompt_counts = torch.full((seqs,), context, dtype=torch.int32, device=self.device)
             rows = torch.randn((seqs, m.heads + 2 * m.kv_heads, m.head_dim), generator=gen, device=self.device).bfloat16()
             self.qkv, (self.q, self.k, self.v) = rows, rows.split([m.heads, m.kv_heads, m.kv_heads], 1)
             self.attended = torch.empty((seqs, m.heads, m.head_dim), dtype=torch.bfloat16, device=self.device)
@@ -60,7 +62,7 @@ class TrustedHalf:
 
     def _prompt(self, gen):
         """Fills the cache with `context` tokens of every sequence."""
-        self._grow(self.context)
+        self._grow(self.context, self.prompt_counts)
         m, n = self.model, self.seqs * self.context
         starts = torch.arange(self.seqs + 1, dtype=torch.int32, device=self.device) * self.context
         for layer in range(self.layers):
@@ -68,8 +70,7 @@ class TrustedHalf:
             bf.bf_kv4_append(self.ctx, self.cache, layer, None, starts, self.seqs, self.context, bf.bf_rows.of(k), bf.bf_rows.of(v))
         bf.bf_trusted_status(self.ctx)
 
-    def _grow(self, tokens: int):
-        counts = None if tokens == 1 else torch.full((self.seqs,), tokens, dtype=torch.int32, device=self.device)
+    def _grow(self, tokens: int, counts=None):
         bf.bf_kv4_grow(self.ctx, self.cache, None, counts, self.seqs)
         self.length += tokens
 
@@ -78,7 +79,7 @@ class TrustedHalf:
         if self.length == self.most:
             bf.bf_kv4_free(self.ctx, self.cache, self.all_seqs, self.seqs)
             self.length = 0
-            self._grow(self.context)
+            self._grow(self.context, self.prompt_counts)
         self._grow(1)
 
     def attend(self, layer: int):
@@ -207,15 +208,25 @@ class WorkloadRunner:
     def step(self):
         """All linear layers of the workload once: the product and its rescale per layer (device buffers), as the one
         call that does both unless the in-ciphertext fold sits between them or the weights come from 4 bits.  With a trusted half,
-        its attention follows the first call of each layer and its projection the last of all."""
+        its attention follows the first call of each layer and its projection the last of all, in that order on whatever streams the
+        two have: one waits for the other, and the step is over when the runner's stream has reached its end."""
         if self.trusted:
-            self.trusted.begin()
+            self._in_turn(self.trusted.begin)
         for i, e in enumerate(self.layers):
             self._call(e)
             if self.trusted and (i == 0 or self.layers[i - 1]["rep"] != e["rep"]):
-                self.trusted.attend(e["rep"])
+                self._in_turn(self.trusted.attend, e["rep"])
         if self.trusted:
-            self.trusted.finish()
+            self._in_turn(self.trusted.finish)
+
+    def _in_turn(self, part, *args):
+        """A part of the trusted half's work behind what the runner's stream has, and before what it gets next."""
+        apart = self.trusted.stream != self.stream
+        if apart:
+            self.trusted.stream.wait_stream(self.stream)
+        part(*args)
+        if apart:
+            self.stream.wait_stream(self.trusted.stream)
 
     def _call(self, e):
         L = e["layer"]

@@ -1059,3 +1059,33 @@ def test_attention_beside_values_that_do_not_count(side, D, G):
         for counts, heads in (([1], 4), ([1], 1), ([2], 4), ([4], 4), ([12], 4)):
             check_attention(side, d, 0, [0], counts, q[:counts[0], :heads], heads, 0, "fp16")
     assert status_of(side) == 0
+
+
+@gpu
+def test_runner_and_trusted_half_on_streams_of_their_own():
+    """Each on its own stream: the cache starts over with the right lengths however busy the runner's stream is, and a step is
+    over on the runner's stream when it is over on both."""
+    import torch
+    from paper_2606_17421_b200.runner import TrustedHalf, WorkloadRunner
+    half = TrustedHalf("gpt2_qkv", seqs=3, context=30, room=2, page_tokens=16)
+    R = WorkloadRunner("gpt2_qkv", trusted=half, q4_group=64)
+    try:
+        assert half.stream != R.stream
+        junk = [torch.full((3,), 7, dtype=torch.int32, device="cuda") for _ in range(50)]    # what the allocator hands out next holds something
+        del junk
+        lens = []
+        for i in range(7):
+            torch.cuda.synchronize()
+            busy, idle = (R.stream, half.stream) if i % 2 == 0 else (half.stream, R.stream)
+            with torch.cuda.stream(busy):
+                torch.cuda._sleep(50_000_000)                                               # 25 ms and more
+            R.step()
+            junk = [torch.full((3,), 9, dtype=torch.int32, device="cuda") for _ in range(50)]
+            del junk
+            R.stream.synchronize()
+            assert half.stream.query()
+            lens.append(half.lengths.tolist())
+        assert lens == [[n] * 3 for n in (31, 32, 31, 32, 31, 32, 31)]
+    finally:
+        R.close()
+        half.close()
