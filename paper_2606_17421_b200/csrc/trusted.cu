@@ -288,13 +288,14 @@ __global__ void __launch_bounds__(COPY_THREADS) free_kernel(Cache c, const int* 
         if (threadIdx.x == 0) atomicOr(status, ST_RANGE);
         return;
     }
-    if (threadIdx.x == 0) claimed = atomicExch(&c.lengths[a], 0);      // one block takes the sequence, others find it empty
+    if (threadIdx.x == 0) {
+        const int len = *static_cast<volatile int*>(c.lengths + a);
+        claimed = 0;
+        if (len < 0 || len > (int)(c.max_pages * c.page_tokens)) atomicOr(status, ST_RANGE);
+        else if (atomicCAS(&c.lengths[a], len, 0) == len) claimed = len;     // one block takes the sequence, others find it empty
+    }
     __syncthreads();
     const int len = claimed;
-    if (len < 0 || len > (int)(c.max_pages * c.page_tokens)) {
-        if (threadIdx.x == 0) atomicOr(status, ST_RANGE);
-        return;
-    }
     int* table = c.tables + (size_t)a * c.max_pages;
     for (int k = threadIdx.x; k < pages_of(len, c.page_tokens); k += COPY_THREADS) {
         const int p = table[k];

@@ -1089,3 +1089,21 @@ def test_runner_and_trusted_half_on_streams_of_their_own():
     finally:
         R.close()
         half.close()
+
+
+@gpu
+def test_free_leaves_a_bad_length_alone(side):
+    """A length out of range is reported; length, table and counts stay, so that nothing is handed out over them."""
+    c = ref.Cache(1, 6, 1, 64, 64, 16, 3, 3)
+    c.grow([0, 1, 2], [20, 16, 40])
+    for length in (-1, -2 ** 31, 49, 2 ** 31 - 1):
+        d = DeviceCache(side, c)
+        d.lengths[0] = length
+        bf.bf_kv4_free(side.t, d.desc, a := side.ints([0, 0, 1]), 3)
+        assert status_of(side) == bf.BF_ERR_RANGE
+        assert side.host(d.lengths).tolist() == [length, 0, 40]
+        tables = c.tables.copy()
+        refs = c.refs.copy()
+        refs[tables[1, 0]] = 0
+        tables[1, 0] = -1
+        assert np.array_equal(side.host(d.tables), tables) and np.array_equal(side.host(d.refs), refs)
