@@ -406,6 +406,7 @@ int bf_kv4_grow(bf_trusted* t, const bf_kv4_cache* c, const int32_t* seqs, const
 /* Quantises rows of k and v ([head][channel], any type) as the last tokens of their sequences in one layer.  Values are clamped to
  * +-61440; scale = (max - min) / 15, low = min, rounded to fp16 by way of fp32; code = round((x - low) / scale), ties to even, decided as in 64
  * bits.  A group with a NaN reads as NaN.  max_new bounds the rows of a sequence (one with more is RANGE and left alone).
+ * Rows that reach back into a page which other sequences name as well are RANGE and not written; the others are.
  * Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
 int bf_kv4_append(bf_trusted* t, const bf_kv4_cache* c, uint32_t layer, const int32_t* seqs, const int32_t* starts, uint32_t n,
                   uint32_t max_new, const bf_rows* k, const bf_rows* v);

@@ -98,7 +98,7 @@ __device__ __forceinline__ uint32_t nibbles_of(uint2 v) {
 }
 
 template <int D, int G>
-__global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned layer, List l, unsigned subs, bf_rows k, bf_rows v, int wide, int* status) {
+__global__ void __launch_bounds__(IO_THREADS, 8) append_kernel(Cache c, unsigned layer, List l, unsigned subs, bf_rows k, bf_rows v, int wide, int* status) {
     using S = Sub<D, G>;
     constexpr int LANES = D / 8, UNITS = IO_THREADS / LANES;                 // lanes of a token; tokens at once
     __shared__ __align__(16) unsigned char image[S::BYTES], code[16 * D];    // code: a byte a nibble of the value words
@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned la
         if (threadIdx.x == 0) atomicOr(status, ST_RANGE);
         return;
     }
+    const int names = threadIdx.x == 0 ? c.refs[page] : 0;                   // (asked for here, needed where the page is written)
     unsigned char* out = c.pool + layer * c.layer_bytes + ((size_t)page * c.heads + head) * c.block_bytes + (t0 % c.page_tokens) / 16 * S::BYTES;
     const int ch = (int)threadIdx.x % LANES * 8, unit = (int)threadIdx.x / LANES;
 #pragma unroll 4
@@ -172,7 +173,10 @@ __global__ void __launch_bounds__(IO_THREADS) append_kernel(Cache c, unsigned la
             p[kind ? 4 : 1] = hm;
         }
     }
-    __syncthreads();
+    if (__syncthreads_or(names > 1)) {                                       // other sequences have it too
+        if (threadIdx.x == 0) atomicOr(status, ST_RANGE);
+        return;
+    }
     if (from == 0 && to == 16) {
         for (int w = threadIdx.x; w < 2 * D; w += IO_THREADS) reinterpret_cast<uint32_t*>(image + S::V_CODE)[w] = nibbles_of(reinterpret_cast<const uint2*>(code)[w]);
         __syncthreads();

@@ -1107,3 +1107,42 @@ def test_free_leaves_a_bad_length_alone(side):
         refs[tables[1, 0]] = 0
         tables[1, 0] = -1
         assert np.array_equal(side.host(d.tables), tables) and np.array_equal(side.host(d.refs), refs)
+
+
+@gpu
+@pytest.mark.parametrize("T", [16, 32])
+def test_append_does_not_write_to_shared_pages(side, T):
+    """Rows that reach back over a branch's own pages: what lies in pages that other sequences name stays, and is reported."""
+    torch, Hk, D = side.torch, 2, 64
+    c = ref.Cache(2, 12, Hk, D, 32, T, 3, 5)
+    d = fill(side, c, [2 * T + 5])
+    bf.bf_kv4_fork(side.t, d.desc, a := side.ints([0, 0]), b := side.ints([1, 2]), 2)
+    c.fork([0, 0], [1, 2])
+    bf.bf_kv4_grow(side.t, d.desc, None, n := side.ints([4, T, 0]), 3)
+    c.grow([0, 1, 2], [4, T, 0])
+    d.same()
+    rng = np.random.default_rng(T)
+    # counts of new rows: the branch's own tokens; exactly to the border; over it; over two borders
+    for counts, code in (([4, T, 1], 0), ([9, T + 5, 5], 0), ([10, 1, 1], bf.BF_ERR_RANGE), ([1, T + 7, 1], bf.BF_ERR_RANGE), ([T + 11, 2, T + 6], bf.BF_ERR_RANGE)):
+        x = rng.standard_normal((sum(counts), 2 * Hk, D)).astype(np.float32)
+        dev = side.dev(x)
+        starts = np.concatenate([[0], np.cumsum(counts)])
+        bf.bf_kv4_append(side.t, d.desc, 1, None, st := side.ints(starts), 3, max(counts), bf.bf_rows.of(dev[:, :Hk]), bf.bf_rows.of(dev[:, Hk:]))
+        for i in range(3):
+            for j in range(counts[i]):
+                t = int(c.lengths[i]) - counts[i] + j
+                if c.refs[c.tables[i, t // T]] == 1:
+                    c.put(1, i, t, x[starts[i] + j, :Hk].astype(np.float64), x[starts[i] + j, Hk:].astype(np.float64))
+        assert status_of(side) == code
+        d.same()
+    # the other branches end: their pages are this one's own
+    bf.bf_kv4_free(side.t, d.desc, e := side.ints([0, 2]), 2)
+    c.free([0, 2])
+    n = int(c.lengths[1])
+    x = rng.standard_normal((n, 2 * Hk, D)).astype(np.float32)
+    dev = side.dev(x)
+    bf.bf_kv4_append(side.t, d.desc, 0, f := side.ints([1]), st := side.ints([0, n]), 1, n, bf.bf_rows.of(dev[:, :Hk]), bf.bf_rows.of(dev[:, Hk:]))
+    for t in range(n):
+        c.put(0, 1, t, x[t, :Hk].astype(np.float64), x[t, Hk:].astype(np.float64))
+    assert status_of(side) == 0
+    d.same()
