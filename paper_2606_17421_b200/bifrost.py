@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libbifrost.so")
@@ -43,40 +44,62 @@ BF_BF16 = 2
 
 
 _ROW_TYPES = {"torch.float32": BF_F32, "torch.float16": BF_F16, "torch.bfloat16": BF_BF16}
-_NAMES = {}                       # torch dtype -> its name, which is slow to make
+_KINDS = {}                       # torch dtype -> its name, which is slow to make, and its type of rows or None
 
 
-def _name(dtype) -> str:
-    name = _NAMES.get(dtype)
-    if name is None:
-        name = _NAMES[dtype] = str(dtype)
-    return name
+def _kind(dtype):
+    name = str(dtype)
+    _KINDS[dtype] = kind = name, _ROW_TYPES.get(name)
+    return kind
 
 
 def _dense(tensor, dtype: str, what: str):
-    if _name(tensor.dtype) != dtype or not tensor.is_contiguous():
+    if (_KINDS.get(tensor.dtype) or _kind(tensor.dtype))[0] != dtype or not tensor.is_contiguous():
         raise ValueError(f"{what}: a contiguous {dtype} tensor is wanted")
     return tensor.data_ptr()
 
 
+def _where(tensor):
+    """The number of the device that a tensor is on, -1 on the host, None where any device reaches it (pinned memory)."""
+    device = tensor.get_device()
+    return device if device >= 0 or not tensor.is_pinned() else None
+
+
+def _common(first, *others):
+    """The device of all of them; -1 where they are not on one."""
+    device = first.get_device()
+    for x in others:
+        if x.get_device() != device:
+            device = -1
+    return device if device >= 0 else -1 if any(_where(x) is not None for x in (first, *others)) else None
+
+
+# Descriptors made of tensors (`of`) keep what calls compare with what they read and write: `device`, and of rows `extent`.  Those made of
+# addresses have neither, and are taken at their word.
+
 class bf_rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
+    __slots__ = ("device", "extent")
 
     @classmethod
     def of(cls, tensor):
         """Rows [n][channels] or [n][heads][channels] of a tensor, which must live as long; any strides but the channels'."""
-        strides, kind = tensor.stride(), _ROW_TYPES.get(_name(tensor.dtype))
+        shape, strides, kind = tensor.shape, tensor.stride(), (_KINDS.get(tensor.dtype) or _kind(tensor.dtype))[1]
         dims = len(strides)
-        if (dims != 3 and dims != 2) or (strides[-1] != 1 and tensor.shape[-1] != 1):
+        if (dims != 3 and dims != 2) or (strides[-1] != 1 and shape[-1] != 1):
             raise ValueError("rows are [n][channels] or [n][heads][channels] with the channels side by side")
         if kind is None:
             raise ValueError(f"rows are float32, float16 or bfloat16, not {tensor.dtype}")
-        return cls(tensor.data_ptr(), strides[0], strides[1] if dims == 3 else 0, kind)
+        rows = cls(tensor.data_ptr(), strides[0], strides[1] if dims == 3 else 0, kind)
+        rows.extent, device = shape, tensor.get_device()
+        rows.device = device if device >= 0 else _where(tensor)
+        return rows
 
 
 class bf_q4_matrix(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("row_bytes", ctypes.c_uint64),
                 ("group_stride", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("d_in", ctypes.c_uint32), ("group", ctypes.c_uint32)]
+    __slots__ = ("device",)
 
     @classmethod
     def of(cls, codes, scales, offsets, d_in: int, group: int):
@@ -86,13 +109,19 @@ class bf_q4_matrix(ctypes.Structure):
             raise ValueError("offsets have the shape of the scales")
         if len(c) != 2 or len(s) != 2 or c[0] != s[0]:
             raise ValueError("codes and scales have a row for each output")
-        return cls(_dense(codes, "torch.uint8", "codes"), _dense(scales, "torch.float16", "scales"),
-                   None if offsets is None else _dense(offsets, "torch.float16", "offsets"), c[1], s[1], c[0], d_in, group)
+        matrix = cls(_dense(codes, "torch.uint8", "codes"), _dense(scales, "torch.float16", "scales"),
+                     None if offsets is None else _dense(offsets, "torch.float16", "offsets"), c[1], s[1], c[0], d_in, group)
+        device = codes.get_device()
+        if device < 0 or scales.get_device() != device or (offsets is not None and offsets.get_device() != device):
+            device = _common(codes, scales) if offsets is None else _common(codes, scales, offsets)
+        matrix.device = device
+        return matrix
 
 
 class bf_kv4_cache(ctypes.Structure):
     _fields_ = [("pool", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p)] + \
                [(name, ctypes.c_uint32) for name in ("n_layers", "n_pages", "n_kv_heads", "head_dim", "group", "page_tokens", "n_seqs", "max_pages")]
+    __slots__ = ("device",)
 
     @classmethod
     def of(cls, pool, tables, lengths, refs, head_dim: int, group: int, page_tokens: int):
@@ -104,8 +133,13 @@ class bf_kv4_cache(ctypes.Structure):
         seqs, n_seqs, n_refs = tables.shape, lengths.shape, refs.shape
         if len(seqs) != 2 or len(n_seqs) != 1 or len(n_refs) != 1 or n_seqs[0] != seqs[0] or n_refs[0] != pages:
             raise BifrostError(BF_ERR_SHAPE, "bf_kv4_cache", "tables, lengths and refs do not fit together")
-        return cls(_dense(pool, "torch.uint8", "pool"), _dense(tables, "torch.int32", "tables"), _dense(lengths, "torch.int32", "lengths"),
-                   _dense(refs, "torch.int32", "refs"), layers, pages, heads, head_dim, group, page_tokens, seqs[0], seqs[1])
+        cache = cls(_dense(pool, "torch.uint8", "pool"), _dense(tables, "torch.int32", "tables"), _dense(lengths, "torch.int32", "lengths"),
+                    _dense(refs, "torch.int32", "refs"), layers, pages, heads, head_dim, group, page_tokens, seqs[0], seqs[1])
+        device = pool.get_device()
+        if device < 0 or tables.get_device() != device or lengths.get_device() != device or refs.get_device() != device:
+            device = _common(pool, tables, lengths, refs)
+        cache.device = device
+        return cache
 
 
 class BifrostError(RuntimeError):
@@ -415,19 +449,60 @@ def _check_trusted(code: int, where: str, t):
         raise BifrostError(code, where, detail)
 
 
-def _ref(struct):
-    return None if struct is None else ctypes.addressof(struct)
+# A context made beside torch knows its device (`own` below, else None), a descriptor made of tensors theirs (None: any).
+
+def _elsewhere(device, own, where: str, what: str):
+    if device is not None and device != own and (device < 0 or own is not None):
+        raise BifrostError(BF_ERR_INVALID_ARG, where, f"{what}: not on the context's device")
 
 
-def _list(x):
-    if x is not None and not isinstance(x, int):
-        return _dense(x, "torch.int32", "a list")
-    return x
+def _ref(struct, own, where: str):
+    if struct is None:
+        return None
+    device = getattr(struct, "device", None)
+    if device != own:
+        _elsewhere(device, own, where, "a descriptor")
+    return ctypes.addressof(struct)
+
+
+def _plain_rows(rows, own, where: str, n: int, width: int):
+    """Looks at n rows without heads, `width` channels side by side."""
+    extent = getattr(rows, "extent", None)
+    if extent is not None:
+        _elsewhere(rows.device, own, where, "rows")
+        if extent[0] < n or (extent[-1] if len(extent) == 2 else (extent[1] - 1) * rows.head_stride + extent[2]) < width:
+            raise BifrostError(BF_ERR_SHAPE, where, f"rows {tuple(extent)} where {n} of {width} channels are wanted")
+
+
+def _head_rows(rows, own, where: str, n: int, heads: int, width: int):
+    """The address of n rows of heads."""
+    if rows is None:
+        return None
+    extent = getattr(rows, "extent", None)
+    if extent is not None:
+        if rows.device != own:
+            _elsewhere(rows.device, own, where, "rows")
+        if extent[0] < n or extent[-1] < width or (extent[1] < heads if len(extent) == 3 else heads > 1):
+            raise BifrostError(BF_ERR_SHAPE, where, f"rows {tuple(extent)} where {n} of {heads} heads of {width} channels are wanted")
+    return ctypes.addressof(rows)
+
+
+def _list(x, own, where: str, n: int, dtype: str = "torch.int32"):
+    if x is None or isinstance(x, int):
+        return x
+    at = _dense(x, dtype, "a list")
+    if x.get_device() != own:
+        _elsewhere(_where(x), own, where, "a list")
+    if x.numel() < n:
+        raise BifrostError(BF_ERR_SHAPE, where, f"a list of {x.numel()} where {n} are wanted")
+    return at
 
 
 def bf_trusted_create(workspace_bytes: int = 0, cuda_stream: int = 0):
     out = _vp()
     _check_trusted(load().bf_trusted_create(ctypes.byref(out), workspace_bytes, cuda_stream), "bf_trusted_create", None)
+    torch = sys.modules.get("torch")
+    out.device = torch.cuda.current_device() if torch else None
     return out
 
 
@@ -441,17 +516,31 @@ def bf_trusted_status(t):
 
 
 def bf_q4_linear(t, W: bf_q4_matrix, x: bf_rows, n: int, y: bf_rows):
-    _check_trusted(load().bf_q4_linear(t, _ref(W), _ref(x), n, _ref(y)), "bf_q4_linear", t)
+    own = getattr(t, "device", None)
+    try:                         # (in one go: the smallest products take as long as their arguments)
+        xs, ys = x.extent, y.extent
+        fits = W.device == own and x.device == own and y.device == own and xs[0] >= n and ys[0] >= n and xs[-1] >= W.d_in and ys[-1] >= W.d_out
+    except AttributeError:
+        fits = False
+    if not fits:
+        _ref(W, own, "bf_q4_linear")
+        _plain_rows(x, own, "bf_q4_linear", n, W.d_in if W else 0)
+        _plain_rows(y, own, "bf_q4_linear", n, W.d_out if W else 0)
+    address = ctypes.addressof
+    code = load().bf_q4_linear(t, W and address(W), x and address(x), n, y and address(y))
+    if code:
+        _check_trusted(code, "bf_q4_linear", t)
 
 
 def bf_encode_weights_q4(ctx, W: bf_q4_matrix, bsgs_b: int = 0, bsgs_g: int = 0):
-    out = _vp()
-    _check(load().bf_encode_weights_q4(ctx, _ref(W), bsgs_b, bsgs_g, ctypes.byref(out)), "bf_encode_weights_q4", ctx)
+    out, where = _vp(), "bf_encode_weights_q4"
+    _check(load().bf_encode_weights_q4(ctx, _ref(W, None, where), bsgs_b, bsgs_g, ctypes.byref(out)), where, ctx)
     return out
 
 
 def bf_linear_q4(ctx, ct_in, n_in: int, W: bf_q4_matrix, ct_out, n_out: int):
-    _check(load().bf_linear_q4(ctx, _ptr(ct_in), n_in, _ref(W), _ptr(ct_out), n_out), "bf_linear_q4", ctx)
+    where = "bf_linear_q4"
+    _check(load().bf_linear_q4(ctx, _ptr(ct_in), n_in, _ref(W, None, where), _ptr(ct_out), n_out), where, ctx)
 
 
 @functools.lru_cache(None)
@@ -459,33 +548,65 @@ def bf_kv4_block_bytes(head_dim: int, group: int, page_tokens: int) -> int:
     return load().bf_kv4_block_bytes(head_dim, group, page_tokens)
 
 
+# (rows that a call reads or writes are known here where each sequence has one: without `starts`)
+
 def bf_kv4_grow(t, cache: bf_kv4_cache, seqs, counts, n: int):
-    _check_trusted(load().bf_kv4_grow(t, _ref(cache), _list(seqs), _list(counts), n), "bf_kv4_grow", t)
+    where, own = "bf_kv4_grow", getattr(t, "device", None)
+    code = load().bf_kv4_grow(t, _ref(cache, own, where), _list(seqs, own, where, n), _list(counts, own, where, n), n)
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_append(t, cache: bf_kv4_cache, layer: int, seqs, starts, n: int, max_new: int, k: bf_rows, v: bf_rows):
-    _check_trusted(load().bf_kv4_append(t, _ref(cache), layer, _list(seqs), _list(starts), n, max_new, _ref(k), _ref(v)), "bf_kv4_append", t)
+    where, own = "bf_kv4_append", getattr(t, "device", None)
+    at, known = _ref(cache, own, where), n if starts is None else 0
+    heads, width = (cache.n_kv_heads, cache.head_dim) if at else (0, 0)
+    code = load().bf_kv4_append(t, at, layer, _list(seqs, own, where, n), _list(starts, own, where, n + 1), n, max_new,
+                                _head_rows(k, own, where, known, heads, width), _head_rows(v, own, where, known, heads, width))
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_read(t, cache: bf_kv4_cache, layer: int, seqs, starts, first, n: int, max_tokens: int, k: bf_rows, v: bf_rows):
-    _check_trusted(load().bf_kv4_read(t, _ref(cache), layer, _list(seqs), _list(starts), _list(first), n, max_tokens, _ref(k), _ref(v)),
-                   "bf_kv4_read", t)
+    where, own = "bf_kv4_read", getattr(t, "device", None)
+    at, known = _ref(cache, own, where), n if starts is None else 0
+    heads, width = (cache.n_kv_heads, cache.head_dim) if at else (0, 0)
+    code = load().bf_kv4_read(t, at, layer, _list(seqs, own, where, n), _list(starts, own, where, n + 1), _list(first, own, where, n), n, max_tokens,
+                              _head_rows(k, own, where, known, heads, width), _head_rows(v, own, where, known, heads, width))
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_attention(t, cache: bf_kv4_cache, layer: int, seqs, starts, n: int, max_q: int, max_len: int, q: bf_rows, n_q_heads: int,
                      out: bf_rows, scale: float, window: int = 0, lse=None):
-    _check_trusted(load().bf_kv4_attention(t, _ref(cache), layer, _list(seqs), _list(starts), n, max_q, max_len, _ref(q), n_q_heads,
-                                           _ref(out), scale, window, None if lse is None else _dense(lse, "torch.float32", "lse")),
-                   "bf_kv4_attention", t)
+    where, own = "bf_kv4_attention", getattr(t, "device", None)
+    at, known = _ref(cache, own, where), n if starts is None else 0
+    width = cache.head_dim if at else 0
+    code = load().bf_kv4_attention(t, at, layer, _list(seqs, own, where, n), _list(starts, own, where, n + 1), n, max_q, max_len,
+                                   _head_rows(q, own, where, known, n_q_heads, width), n_q_heads, _head_rows(out, own, where, known, n_q_heads, width),
+                                   scale, window, _list(lse, own, where, known * n_q_heads, "torch.float32"))
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_fork(t, cache: bf_kv4_cache, src, dst, n: int):
-    _check_trusted(load().bf_kv4_fork(t, _ref(cache), _list(src), _list(dst), n), "bf_kv4_fork", t)
+    where, own = "bf_kv4_fork", getattr(t, "device", None)
+    code = load().bf_kv4_fork(t, _ref(cache, own, where), _list(src, own, where, n), _list(dst, own, where, n), n)
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_free(t, cache: bf_kv4_cache, seqs, n: int):
-    _check_trusted(load().bf_kv4_free(t, _ref(cache), _list(seqs), n), "bf_kv4_free", t)
+    where, own = "bf_kv4_free", getattr(t, "device", None)
+    code = load().bf_kv4_free(t, _ref(cache, own, where), _list(seqs, own, where, n), n)
+    if code:
+        _check_trusted(code, where, t)
 
 
 def bf_kv4_compact(t, cache: bf_kv4_cache, tables_out=None, refs_out=None, n_live=None):
-    _check_trusted(load().bf_kv4_compact(t, _ref(cache), _list(tables_out), _list(refs_out), _list(n_live)), "bf_kv4_compact", t)
+    where, own = "bf_kv4_compact", getattr(t, "device", None)
+    at = _ref(cache, own, where)
+    entries, pages = (cache.n_seqs * cache.max_pages, cache.n_pages) if at else (0, 0)
+    code = load().bf_kv4_compact(t, at, _list(tables_out, own, where, entries), _list(refs_out, own, where, pages), _list(n_live, own, where, 1))
+    if code:
+        _check_trusted(code, where, t)

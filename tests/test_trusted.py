@@ -1146,3 +1146,113 @@ def test_append_does_not_write_to_shared_pages(side, T):
         c.put(0, 1, t, x[t, :Hk].astype(np.float64), x[t, Hk:].astype(np.float64))
     assert status_of(side) == 0
     d.same()
+
+
+class Held:
+    """A tensor as one on a device looks to the binding: nothing behind its address."""
+
+    def __init__(self, like, device=0):
+        self.like, self.device_index, self.dtype, self.shape = like, device, like.dtype, like.shape
+
+    def get_device(self):
+        return self.device_index
+
+    def data_ptr(self):
+        return 4096
+
+    def stride(self):
+        return self.like.stride()
+
+    def numel(self):
+        return self.like.numel()
+
+    def is_contiguous(self):
+        return self.like.is_contiguous()
+
+    def is_pinned(self):
+        return False
+
+
+def test_calls_refuse_tensors_that_are_too_small(stand_in):
+    """What descriptors and lists are made of is compared with what a call reads and writes."""
+    torch = pytest.importorskip("torch")
+    z = lambda *shape, type=torch.bfloat16: Held(torch.zeros(shape, dtype=type))       # noqa: E731
+    ints = lambda *shape: z(*shape, type=torch.int32)                                  # noqa: E731
+    R = bf.bf_rows.of
+    W = bf.bf_q4_matrix.of(z(50, 48, type=torch.uint8), z(50, 8, type=torch.float16), None, 90, 32)
+    lin = lambda x, n, y: refused(bf.BF_ERR_SHAPE, bf.bf_q4_linear, stand_in, W, R(x), n, R(y))    # noqa: E731
+    lin(z(4, 90), 5, z(5, 50))                                                         # rows of x, of y
+    lin(z(5, 90), 5, z(4, 50))
+    lin(z(5, 89), 5, z(5, 50))                                                         # columns of x, of y
+    lin(z(5, 90), 5, z(5, 49))
+    lin(z(5, 3, 29), 5, z(5, 50))
+    lin(z(5, 3, 30), 5, z(5, 2, 24))
+    c = bf.bf_kv4_cache.of(z(2, 8, 3, 64 * 16 + 256, type=torch.uint8), ints(4, 5), ints(4), ints(8), 64, 32, 16)
+    good = z(6, 3, 64)
+    for bad in (z(3, 3, 64), z(6, 2, 64), z(6, 3, 63), z(6, 64), z(6, 192)):
+        for k, v in ((good, bad), (bad, good)):
+            refused(bf.BF_ERR_SHAPE, bf.bf_kv4_append, stand_in, c, 0, None, None, 4, 1, R(k), R(v))
+            refused(bf.BF_ERR_SHAPE, bf.bf_kv4_read, stand_in, c, 0, None, None, None, 4, 1, R(k), R(v))
+    query = z(6, 6, 64)
+    for bad in (z(3, 6, 64), z(6, 5, 64), z(6, 6, 60), z(6, 384)):
+        for q, out in ((query, bad), (bad, query)):
+            refused(bf.BF_ERR_SHAPE, bf.bf_kv4_attention, stand_in, c, 0, None, None, 4, 1, 50, R(q), 6, R(out), 1.0, 0, None)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_attention, stand_in, c, 0, None, None, 4, 1, 50, R(query), 6, R(query), 1.0, 0, z(4, 5, type=torch.float32))
+    # lists: seqs of n, starts of n + 1, counts and first of n
+    for seqs, starts in ((ints(3), None), (None, ints(4)), (ints(4), ints(4)), (ints(2, 1), ints(5))):
+        refused(bf.BF_ERR_SHAPE, bf.bf_kv4_append, stand_in, c, 0, seqs, starts, 4, 1, R(good), R(good))
+        refused(bf.BF_ERR_SHAPE, bf.bf_kv4_read, stand_in, c, 0, seqs, starts, None, 4, 1, R(good), R(good))
+        refused(bf.BF_ERR_SHAPE, bf.bf_kv4_attention, stand_in, c, 0, seqs, starts, 4, 1, 50, R(query), 6, R(query), 1.0, 0, None)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_read, stand_in, c, 0, None, None, ints(3), 4, 1, R(good), R(good))
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_grow, stand_in, c, ints(3), None, 4)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_grow, stand_in, c, None, ints(3), 4)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_fork, stand_in, c, ints(1), ints(2), 2)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_fork, stand_in, c, ints(2), ints(1), 2)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_free, stand_in, c, ints(1), 2)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_compact, stand_in, c, ints(4, 4), None, None)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_compact, stand_in, c, None, ints(7), None)
+    refused(bf.BF_ERR_SHAPE, bf.bf_kv4_compact, stand_in, c, None, None, ints(0))
+
+
+def test_calls_refuse_tensors_that_are_elsewhere(stand_in):
+    """On the host, or on another device than the context's."""
+    torch = pytest.importorskip("torch")
+    inv = bf.BF_ERR_INVALID_ARG
+    t = ctypes.c_void_p(ctypes.addressof(stand_in))
+    t.device = 0
+    z = lambda *shape, type=torch.bfloat16: torch.zeros(shape, dtype=type)             # noqa: E731
+    R, Z = bf.bf_rows.of, torch.int32
+    for at in (lambda x: x, lambda x: Held(x, 1)):
+        for where in range(4):
+            on = lambda i, x: at(x) if i == where else Held(x)                         # noqa: E731
+            W = bf.bf_q4_matrix.of(on(0, z(50, 48, type=torch.uint8)), on(1, z(50, 8, type=torch.float16)), None, 90, 32)
+            refused(inv, bf.bf_q4_linear, t, W, R(on(2, z(1, 90))), 1, R(on(3, z(1, 50))))
+        for where in range(10):
+            c = bf.bf_kv4_cache.of(on(0, z(2, 8, 3, 64 * 16 + 256, type=torch.uint8)), on(1, z(4, 5, type=Z)), on(2, z(4, type=Z)), on(3, z(8, type=Z)), 64, 32, 16)
+            q, out, lse = R(on(4, z(6, 3, 64))), R(on(5, z(6, 3, 64))), on(6, z(6, 3, type=torch.float32))
+            seqs, starts, first = on(7, z(4, type=Z)), on(8, z(5, type=Z)), on(9, z(4, type=Z))
+            if where < 9:
+                refused(inv, bf.bf_kv4_attention, t, c, 0, seqs, starts, 4, 1, 50, q, 3, out, 1.0, 0, lse)
+            if where != 6:
+                refused(inv, bf.bf_kv4_read, t, c, 0, seqs, starts, first, 4, 1, q, out)
+            if where < 9 and where != 6:
+                refused(inv, bf.bf_kv4_append, t, c, 0, seqs, starts, 4, 1, q, out)
+            if where in (0, 1, 2, 3, 7, 9):
+                refused(inv, bf.bf_kv4_grow, t, c, seqs, first, 4)
+                refused(inv, bf.bf_kv4_fork, t, c, seqs, first, 4)
+            if where in (0, 1, 2, 3, 7):
+                refused(inv, bf.bf_kv4_free, t, c, seqs, 4)
+            if where < 4:
+                refused(inv, bf.bf_kv4_compact, t, c)
+        c = bf.bf_kv4_cache.of(Held(z(2, 8, 3, 64 * 16 + 256, type=torch.uint8)), Held(z(4, 5, type=Z)), Held(z(4, type=Z)), Held(z(8, type=Z)), 64, 32, 16)
+        for tables, refs, live in ((at(z(4, 5, type=Z)), None, None), (None, at(z(8, type=Z)), None), (None, None, at(z(1, type=Z)))):
+            refused(inv, bf.bf_kv4_compact, t, c, tables, refs, live)
+
+
+def test_calls_refuse_no_cache(stand_in):
+    r, inv = rows(), bf.BF_ERR_INVALID_ARG
+    refused(inv, bf.bf_kv4_append, stand_in, None, 0, None, None, 1, 1, r, r)
+    refused(inv, bf.bf_kv4_read, stand_in, None, 0, None, None, None, 1, 1, r, r)
+    refused(inv, bf.bf_kv4_attention, stand_in, None, 0, None, None, 1, 1, 1, r, 1, r, 1.0)
+    refused(inv, bf.bf_kv4_compact, stand_in, None)
+    refused(inv, bf.bf_kv4_grow, stand_in, None, None, None, 1)
