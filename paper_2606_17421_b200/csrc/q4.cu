@@ -280,7 +280,9 @@ __global__ void __launch_bounds__(MOST_WARPS * 32) q4_few_kernel(Q4 w, bf_rows x
                     }
                 }
                 const float2 un = *reinterpret_cast<const float2*>(undo + seg * 8 + 2 * j);
-                total[0] += un.x * part[0], total[1] += un.y * part[1], total[2] += un.x * part[2], total[3] += un.y * part[3];
+                // (2^24 first: with x near the end of the range on either side, what is undone by itself would leave it)
+                total[0] += un.x * (part[0] * 0x1p24f), total[1] += un.y * (part[1] * 0x1p24f);
+                total[2] += un.x * (part[2] * 0x1p24f), total[3] += un.y * (part[3] * 0x1p24f);
                 __syncwarp();                                    // the slot is free for the next copy
                 slot = slot + 1 == STAGES ? 0 : slot + 1;
             }
@@ -298,14 +300,14 @@ __global__ void __launch_bounds__(MOST_WARPS * 32) q4_few_kernel(Q4 w, bf_rows x
             const unsigned o = tile * 16 + g;
             if (x.type == BF_F32) {
                 if (2 * j < cols) {
-                    if (o < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o, (total[0] + total[1]) * 0x1p24f);
-                    if (o + 8 < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o + 8, (total[2] + total[3]) * 0x1p24f);
+                    if (o < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o, total[0] + total[1]);
+                    if (o + 8 < w.d_out) store_from_float(y.data, y.type, (int64_t)j * y.row_stride + o + 8, total[2] + total[3]);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const unsigned col = 2 * j + i % 2, row = o + i / 2 * 8;
-                    if (col < cols && row < w.d_out) store_from_float(y.data, y.type, (int64_t)col * y.row_stride + row, total[i] * 0x1p24f);
+                    if (col < cols && row < w.d_out) store_from_float(y.data, y.type, (int64_t)col * y.row_stride + row, total[i]);
                 }
             }
         }
@@ -570,12 +572,12 @@ __global__ void __launch_bounds__(MANY_WARPS * 32, NT <= 4 ? 2 : 1) q4_many_kern
                 for (int i = 0; i < 4; ++i) {                    // four rows of 16 m + 8 h + g
                     const unsigned o = tile * ROWS + 8 * i + g;
                     if (o >= w.d_out) continue;
-                    const float a = total[i / 2][t][i % 2 * 2] * u0, b = total[i / 2][t][i % 2 * 2 + 1] * u1;
+                    const float a = total[i / 2][t][i % 2 * 2] * 0x1p24f * u0, b = total[i / 2][t][i % 2 * 2 + 1] * 0x1p24f * u1;
                     if (two) {
-                        store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, (a + b) * 0x1p24f);
+                        store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, a + b);
                     } else {
-                        store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, a * 0x1p24f);
-                        if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, b * 0x1p24f);
+                        store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, a);
+                        if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, b);
                     }
                 }
             }
@@ -844,12 +846,12 @@ __global__ void __launch_bounds__(TILE, N == 64 || Wide<G, OFFSETS, N>::TMEM > 1
             for (int c = 0; c < N; c += 2) {
                 const unsigned col = blockIdx.y * N + c;
                 if (col >= n_cols) break;
-                const float u = total[c] * p.undo[col], v = col + 1 < n_cols ? total[c + 1] * p.undo[col + 1] : 0.f;
+                const float u = total[c] * 0x1p24f * p.undo[col], v = col + 1 < n_cols ? total[c + 1] * 0x1p24f * p.undo[col + 1] : 0.f;
                 if (two) {
-                    store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, (u + v) * 0x1p24f);
+                    store_from_float(y.data, y.type, (int64_t)(row0 + col / 2) * y.row_stride + o, u + v);
                 } else {
-                    store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, u * 0x1p24f);
-                    if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, v * 0x1p24f);
+                    store_from_float(y.data, y.type, (int64_t)(row0 + col) * y.row_stride + o, u);
+                    if (col + 1 < n_cols) store_from_float(y.data, y.type, (int64_t)(row0 + col + 1) * y.row_stride + o, v);
                 }
             }
         }

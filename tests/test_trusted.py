@@ -1256,3 +1256,23 @@ def test_calls_refuse_no_cache(stand_in):
     refused(inv, bf.bf_kv4_attention, stand_in, None, 0, None, None, 1, 1, 1, r, 1, r, 1.0)
     refused(inv, bf.bf_kv4_compact, stand_in, None)
     refused(inv, bf.bf_kv4_grow, stand_in, None, None, None, 1)
+
+
+@gpu
+@pytest.mark.parametrize("n,d_out", [(1, 48), (3, 48), (20, 48), (20, 19000), (64, 2400)])
+def test_linear_of_values_near_the_end_of_the_range(side, n, d_out):
+    """x next to the smallest normal number, and so large that only the weights bring y back into range: results are normal
+    numbers and as exact as any."""
+    torch = side.torch
+    for xt, size in itertools.product(("fp32", "bf16"), (2.0 ** -110, 2.0 ** -119, 2.0 ** -123, 2.0 ** 121)):
+        rng = np.random.default_rng([n, d_out])
+        packed, scales, _, W, top = draw_matrix(rng, d_out, 300, 32, False)
+        codes, sc = side.dev(packed), side.dev(scales)
+        x = (torch.from_numpy(rng.standard_normal((n, 300))) * size).to(side.types[xt]).cuda()
+        y = torch.empty((n, d_out), device="cuda")
+        bf.bf_q4_linear(side.t, bf.bf_q4_matrix.of(codes, sc, None, 300, 32), bf.bf_rows.of(x), n, bf.bf_rows.of(y))
+        xd, got = side.host(x), side.host(y)
+        want = xd @ W.T
+        # (a sum below the normal range, 2^-126, may be rounded to that range's last place at each of its steps)
+        tol = linear_tolerance(xd, want, top, "fp32") + 64 * 2.0 ** -149
+        assert (np.abs(got - want) <= tol).all(), (xt, size, np.abs(got - want).max() / size)
