@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
     // one column of rows: scales go to p, 5 instructions for 8 codes.  More: values are made once for all, 13 for 8.
     constexpr bool SCALE_P = NT == 1;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float sh_m[ATT_WARPS][RW], sh_l[ATT_WARPS][RW], row_scale[RW];
+    __shared__ float sh_m[ATT_WARPS][RW], sh_l[ATT_WARPS][RW], row_scale[RW], row_lift[RW];
     __shared__ unsigned last;
     uint4* qf = reinterpret_cast<uint4*>(smem);                              // [BLOCKS][RW][4]
     float* qs = reinterpret_cast<float*>(smem + BLOCKS * RW * 64);           // [E][RW] sums of q * 2^-24
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
         for (int d = 16; d; d >>= 1) big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
         // 2^k with 2^14 <= big 2^k < 2^15, where 2^k is a float
         const int e = max(1, (int)(__float_as_uint(big) >> 23));
-        const float up = __uint_as_float((unsigned)min(253, 268 - e) << 23), down = __uint_as_float((unsigned)max(1, e - 14) << 23);
+        const float up = __uint_as_float((unsigned)min(253, 268 - e) << 23);
         float h[8], sum = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -540,7 +540,15 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
 #pragma unroll
         for (int d = G / 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
         if (lane < D / 8 && lane % (G / 8) == 0) qs[lane / (G / 8) * RW + r] = sum * 0x1p-24f;
-        if (lane == 0) row_scale[r] = p.scale * 1.4426950408889634f * (down * 0x1p24f);
+        if (lane == 0) {
+            // Scores are x times this, below 2^101: with more, x of 2^14 leaves the range before the score does.  What is taken off makes a difference
+            // to none but the log-sum-exp, since scores that differ at all are then 2^20 and more apart.
+            const float c = p.scale * 1.4426950408889634f;
+            const int by = max(1, e - 14) - 127 + 24, off = min(127, max(0, (int)(__float_as_uint(c) >> 23 & 255) - 127 + by - 100));
+            const int half = (by - off) / 2, rest = by - off - half;        // (all of it may be above 2^127)
+            row_scale[r] = c * __int_as_float((127 + rest) << 23) * __int_as_float((127 + half) << 23);
+            row_lift[r] = __int_as_float((127 + off) << 23);
+        }
     }
     __syncthreads();
 
@@ -844,7 +852,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
             const float inv = sum == 0 ? 0.f : 1.f / sum;
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) store_from_float(p.out.data, p.out.type, row * p.out.row_stride + head * p.out.head_stride + lane + 32 * k, y[k] * inv);
-            if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+            if (p.lse && lane == 0) p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top * row_lift[r] + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
         } else {
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) part[r * D + lane + 32 * k] = y[k];
@@ -882,7 +890,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, NT == 1 ? 2 : 1) attention_ker
                 unsigned h;
                 const unsigned j = p.per.split(r0 + r, h);
                 const int64_t row = s.row0 + (int)j, head = kv * per + h;
-                p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
+                p.lse[row * p.q_heads + head] = sum == 0 ? -CUDART_INF_F : (top * row_lift[r] + log2f(sum) - (float)P_UP) * 0.69314718055994531f;
             }
         }
     }

@@ -1276,3 +1276,59 @@ def test_linear_of_values_near_the_end_of_the_range(side, n, d_out):
         # (a sum below the normal range, 2^-126, may be rounded to that range's last place at each of its steps)
         tol = linear_tolerance(xd, want, top, "fp32") + 64 * 2.0 ** -149
         assert (np.abs(got - want) <= tol).all(), (xt, size, np.abs(got - want).max() / size)
+
+
+def random_tokens(c, lens, seed=0):
+    """Sequences of these lengths with any codes and parameters as ordinary keys and values have them, made at once."""
+    rng = np.random.default_rng(seed)
+    c.grow(list(range(len(lens))), list(lens))
+    c.pool[:] = rng.integers(0, 256, c.pool.shape, dtype=np.uint8)
+    half = c.pool.view(np.float16)
+    for par, low_at in ((c.kp, 1), (c.vp, 4)):
+        at = np.unique(par)
+        half[..., at] = rng.uniform(0.1, 0.4, (*c.pool.shape[:4], at.size)).astype(np.float16)
+        half[..., at + low_at] = rng.uniform(-3, -1, (*c.pool.shape[:4], at.size)).astype(np.float16)
+
+
+@gpu
+@pytest.mark.parametrize("D,G", [(64, 32), (128, 128)])
+def test_attention_of_queries_near_the_end_of_the_range(side, D, G):
+    """Scores of 10^36: finite in 32 bits, so the token with the largest is the answer, and log-sum-exp is its score."""
+    torch = side.torch
+    for length in (50, 5000):
+        c = ref.Cache(1, length // 16 + 2, 1, D, G, 16, 1, length // 16 + 1)
+        random_tokens(c, [length])
+        d = DeviceCache(side, c)
+        k, v = c.get(0, 0, length)
+        vt = c.top(0, 0, length)[1]
+        for size in (2.0 ** 80, 2.0 ** 110, 2.0 ** 119, 2.0 ** 122):
+            q = (torch.randn((12, 2, D), device="cuda") * size).bfloat16()
+            qd = side.host(q)
+            for rows in (1, 3, 12):
+                st = side.ints([0, rows])
+                out, lse = torch.zeros((rows, 2, D), device="cuda").bfloat16(), torch.zeros((rows, 2), device="cuda")
+                bf.bf_kv4_attention(side.t, d.desc, 0, None, st, 1, rows, length, bf.bf_rows.of(q[:rows]), 2, bf.bf_rows.of(out), D ** -0.5, 0, lse)
+                o, l = side.host(out), side.host(lse)
+                for j, h in itertools.product(range(rows), range(2)):
+                    n = length - rows + j + 1
+                    s = D ** -0.5 * (k[:n, 0] @ qd[j, h])
+                    at = int(s.argmax())
+                    # (next to a tie the answer is a mixture; none of these are: gaps are 10^30 and more)
+                    assert np.abs(o[j, h] - v[at, 0]).max() <= (2.0 ** -8 + 2.0 ** -10) * vt[at, 0].max(), (length, size, rows)
+                    assert abs(l[j, h] - s[at]) <= 2.0 ** -16 * np.abs(s).max()
+    assert status_of(side) == 0
+
+
+@gpu
+def test_attention_scale_that_brings_scores_back_into_range(side):
+    """q beyond what a score could be, a scale as small: ordinary scores, and the other way round."""
+    torch = side.torch
+    c = ref.Cache(1, 10, 2, 64, 32, 16, 1, 8)
+    random_tokens(c, [100])
+    d = DeviceCache(side, c)
+    base = torch.randn((5, 4, 64), device="cuda")
+    for e in (-100, -60, 60, 100, 114, 122):
+        q = (base * 2.0 ** e).bfloat16()
+        for rows in (1, 5):
+            check_attention(side, d, 0, [0], [rows], q[:rows], 4, 0, "bf16", scale=0.125 * 2.0 ** -e)
+    assert status_of(side) == 0
