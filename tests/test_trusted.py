@@ -1332,3 +1332,23 @@ def test_attention_scale_that_brings_scores_back_into_range(side):
         for rows in (1, 5):
             check_attention(side, d, 0, [0], [rows], q[:rows], 4, 0, "bf16", scale=0.125 * 2.0 ** -e)
     assert status_of(side) == 0
+
+
+@pytest.mark.parametrize("name,fused,calls", [("qwen3_step", False, ["q", "k", "v", "*", "o", "gate", "up", "down"]), ("qwen3_step", True, ["q+k+v", "*", "o", "gate+up", "down"]),
+                                              ("gpt2_step", True, ["qkv", "*", "out_proj", "ffn_up", "ffn_down"]), ("gpt2_qkv", True, ["qkv", "*"]),
+                                              ("llama3_layer", False, ["q", "k", "v", "*", "o", "gate", "up", "down"])])
+def test_attention_follows_q_k_and_v(name, fused, calls):
+    """The order of a step's work, stacked projections or not: attention of a layer once all it reads is there."""
+    from types import SimpleNamespace
+
+    from paper_2606_17421_b200 import workloads as wl
+    from paper_2606_17421_b200.runner import WorkloadRunner
+    w = wl.WORKLOADS[name]
+    units = [wl.Layer(nm, d_in, 0, ms[0].input) for nm, d_in, ms in wl.fuse_shared_inputs(w.layers, w.plan.D)] if fused else w.layers
+    R, did = WorkloadRunner.__new__(WorkloadRunner), []
+    R.layers = [dict(layer=L, rep=rep) for rep in range(w.n_repeat) for L in units]
+    R.stream = "one"
+    R.trusted = SimpleNamespace(stream="one", begin=lambda: did.append("<"), attend=lambda rep: did.append(("*", rep)), finish=lambda: did.append(">"))
+    R._call = lambda e: did.append((e["layer"].name, e["rep"]))
+    R.step()
+    assert did == ["<"] + [(c, rep) for rep in range(w.n_repeat) for c in calls] + [">"]
