@@ -209,24 +209,30 @@ class WorkloadRunner:
         """All linear layers of the workload once: the product and its rescale per layer (device buffers), as the one
         call that does both unless the in-ciphertext fold sits between them or the weights come from 4 bits.  With a trusted half,
         its attention follows the products of each layer that make q, k and v (the first, and those that read the same input) and its
-        projection the last of all, in that order on whatever streams the two have: one waits for the other, and the step is over when the runner's stream has reached its end."""
+        projection the last of all, in that order on whatever streams the two have: one waits for the other, and the step is over when
+        the runner's stream has reached its end."""
+        after = self._ends_of_qkv() if self.trusted else ()
         if self.trusted:
             self._in_turn(self.trusted.begin)
         for i, e in enumerate(self.layers):
             self._call(e)
-            if self.trusted and self._makes_qkv(i) and not self._makes_qkv(i + 1):
+            if i in after:
                 self._in_turn(self.trusted.attend, e["rep"])
         if self.trusted:
             self._in_turn(self.trusted.finish)
 
-    def _makes_qkv(self, i: int) -> bool:
-        """Call i is the first of its transformer layer, or one in a row with it that reads the same input."""
-        if i == len(self.layers):
-            return False
-        e = self.layers[i]
-        if i == 0 or self.layers[i - 1]["rep"] != e["rep"]:
-            return True
-        return e["layer"].input != "" and self.layers[i - 1]["layer"].input == e["layer"].input and self._makes_qkv(i - 1)
+    def _ends_of_qkv(self):
+        """The calls with which q, k and v of a transformer layer are there: of those at its start that read one input, the last."""
+        ends, rep, tag = [], None, ""
+        for i, e in enumerate(self.layers):
+            if e["rep"] != rep:
+                rep, tag = e["rep"], e["layer"].input
+                ends.append(i)
+            elif tag and e["layer"].input == tag:
+                ends[-1] = i
+            else:
+                tag = ""
+        return set(ends)
 
     def _in_turn(self, part, *args):
         """A part of the trusted half's work behind what the runner's stream has, and before what it gets next."""

@@ -1352,3 +1352,19 @@ def test_attention_follows_q_k_and_v(name, fused, calls):
     R._call = lambda e: did.append((e["layer"].name, e["rep"]))
     R.step()
     assert did == ["<"] + [(c, rep) for rep in range(w.n_repeat) for c in calls] + [">"]
+
+
+def test_attention_of_layers_with_one_input():
+    """Layers that are nothing but q, k and v, one after the other."""
+    from types import SimpleNamespace
+
+    from paper_2606_17421_b200 import workloads as wl
+    from paper_2606_17421_b200.runner import WorkloadRunner
+    for units in ([wl.Layer("qkv", 8, 24)], [wl.Layer(x, 8, 8, "attn") for x in "qkv"]):
+        R, did = WorkloadRunner.__new__(WorkloadRunner), []
+        R.layers = [dict(layer=L, rep=rep) for rep in range(3) for L in units]
+        R.stream = "one"
+        R.trusted = SimpleNamespace(stream="one", begin=lambda: None, attend=lambda rep: did.append("*"), finish=lambda: None)
+        R._call = lambda e: did.append(e["layer"].name)
+        R.step()
+        assert did == ([L.name for L in units] + ["*"]) * 3
