@@ -29,6 +29,8 @@ class TrustedHalf:
 
     def __init__(self, name: str, seqs: int = 1, context: int = 512, room: int = 512, group: int = 64, page_tokens: int = 64, seed: int = 0,
                  device: str = "cuda:0", stream: torch.cuda.Stream | None = None):
+        if seqs < 1 or context < 1 or room < 1:
+            raise ValueError("a sequence, a token of its prompt and room for a step's token are the least")
         m = self.model = wl.DECODERS[name]
         self.layers, self.seqs, self.context, self.most = wl.WORKLOADS[name].n_repeat, seqs, context, context + room
         self.device = torch.device(device)
@@ -94,8 +96,11 @@ class TrustedHalf:
         bf.bf_q4_linear(self.ctx, self.head, bf.bf_rows.of(self.hidden), self.seqs, bf.bf_rows.of(self.logits))
 
     def close(self):
-        bf.bf_trusted_status(self.ctx)
-        bf.bf_trusted_destroy(self.ctx)
+        """Raises what the kernels found wrong; the context is gone either way."""
+        try:
+            bf.bf_trusted_status(self.ctx)
+        finally:
+            bf.bf_trusted_destroy(self.ctx)
 
 
 class WorkloadRunner:

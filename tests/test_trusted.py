@@ -1368,3 +1368,21 @@ def test_attention_of_layers_with_one_input():
         R._call = lambda e: did.append(e["layer"].name)
         R.step()
         assert did == ([L.name for L in units] + ["*"]) * 3
+
+
+def test_trusted_half_refuses_and_ends(monkeypatch):
+    """No room for a step's token is refused before anything is made; a context that found something wrong is destroyed all the same."""
+    from paper_2606_17421_b200.runner import TrustedHalf
+    for kw in (dict(room=0), dict(seqs=0), dict(context=0), dict(room=-1)):
+        with pytest.raises(ValueError):
+            TrustedHalf("gpt2_qkv", **kw)
+    half, gone = TrustedHalf.__new__(TrustedHalf), []
+    half.ctx = "context"
+
+    def found(t):
+        raise bf.BifrostError(bf.BF_ERR_RANGE, "bf_trusted_status")
+
+    monkeypatch.setattr(bf, "bf_trusted_status", found)
+    monkeypatch.setattr(bf, "bf_trusted_destroy", gone.append)
+    refused(bf.BF_ERR_RANGE, half.close)
+    assert gone == ["context"]
