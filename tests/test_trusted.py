@@ -1386,3 +1386,111 @@ def test_trusted_half_refuses_and_ends(monkeypatch):
     monkeypatch.setattr(bf, "bf_trusted_destroy", gone.append)
     refused(bf.BF_ERR_RANGE, half.close)
     assert gone == ["context"]
+
+
+def product_in_64_bits(torch, codes, scales, offs, d_in, group, x):
+    """(y, what linear_tolerance's `top` gives for |x|, and for the largest of a row), by pieces on the device."""
+    col = torch.arange(d_in, device="cuda")
+    ys, mags, bigs = [], [], []
+    xd = x.double()
+    for at in range(0, codes.shape[0], 2048):
+        some = slice(at, at + 2048)
+        code = (codes[some][:, col // 2].int() >> (4 * (col % 2)) & 15).double()
+        s = scales[some][:, col // group].double()
+        z = offs[some][:, col // group].double() if offs is not None else torch.zeros_like(s)
+        ys.append(xd @ (s * (code - 8) + z).t())
+        top = s * 23 + z.abs()
+        mags.append(xd.abs() @ top.t())
+        bigs.append(xd.abs().amax(1, keepdim=True) * top.sum(1))
+    return [torch.cat(a, 1).cpu().numpy() for a in (ys, mags, bigs)]
+
+
+def check_product(side, t, n, d_in, d_out, group, offsets, xt, yt, strided=False, x=None, seed=0):
+    torch = side.torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    groups = -(-d_in // group)
+    codes = torch.randint(0, 256, (d_out, -(-d_in // 32) * 16), generator=gen, device="cuda", dtype=torch.uint8)
+    scales = (torch.rand((d_out, -(-groups // 8) * 8), generator=gen, device="cuda") * 0.009 + 0.001).half()
+    offs = (torch.randn(scales.shape, generator=gen, device="cuda") * 0.02).half() if offsets else None
+    for a in (scales, offs):
+        if a is not None:
+            a[:, groups:] = float("nan")
+    if x is None:
+        x = torch.randn((n, d_in), generator=gen, device="cuda")
+    x = x.to(side.types[xt])
+    pad = torch.full((n + 1, d_out + 11), 5.0, device="cuda").to(side.types[yt])
+    if strided:                                                                              # odd strides, odd starts
+        x, y = torch.nn.functional.pad(x, (7, 2))[:, 7:7 + d_in], pad[:, 3:3 + d_out]
+    else:
+        y = pad[:, :d_out]
+    bf.bf_q4_linear(t, bf.bf_q4_matrix.of(codes, scales, offs, d_in, group), bf.bf_rows.of(x), n, bf.bf_rows.of(y))
+    want, mag, big = product_in_64_bits(torch, codes, scales, offs, d_in, group, x)
+    got, at = side.host(y), 3 if strided else 0
+    tol = HALF_STEP[yt] * np.abs(want) + 2.0 ** -22 * (d_in / 16 + d_in / 32 + 24) * mag + 2.0 ** -24 * big + TINY[yt]
+    fine = np.isfinite(side.host(x)).all(1)
+    assert (np.abs(got[:n] - want)[fine] <= tol[fine]).all(), (np.abs(got[:n] - want) - tol)[fine].max()
+    assert not np.isfinite(got[:n][~fine]).any()
+    rest = side.host(pad)
+    assert (rest[n] == 5).all() and (rest[:, :at] == 5).all() and (rest[:, at + d_out:] == 5).all()
+
+
+WIDE = [(12, 333, 19001, 64), (20, 600, 18950, 32), (30, 1000, 19000, 128), (64, 333, 2400, 128), (100, 520, 2401, 64)]
+
+
+@gpu
+@pytest.mark.parametrize("n,d_in,d_out,group", WIDE)
+def test_linear_of_many_outputs_strided(side, n, d_in, d_out, group):
+    """Rows without alignment through the products of 128 rows of W at a time."""
+    for i, (xt, yt) in enumerate((("bf16", "fp32"), ("fp32", "fp16"), ("fp16", "bf16"))):
+        if xt == "fp32" and d_out > 18000:
+            n = max(n // 2, 9)
+        check_product(side, side.t, n, d_in, d_out, group, i == 1, xt, yt, strided=True, seed=i)
+    bf.bf_trusted_status(side.t)
+
+
+@gpu
+@pytest.mark.parametrize("n,d_in,d_out,group", WIDE)
+def test_linear_of_many_outputs_with_extreme_rows(side, n, d_in, d_out, group):
+    """Rows of zeros, tiny and huge values; NaN and infinities stay in their rows."""
+    torch = side.torch
+    for xt in ("fp32", "bf16", "fp16"):
+        rows = n // 2 if xt == "fp32" else n
+        x = torch.randn((rows, d_in), device="cuda")
+        x[0] = 0
+        if xt != "fp16":
+            x[1] *= 1e-30
+            x[2] *= 1e30
+        x[3, ::7] *= 1e3
+        x[4, d_in - 1] = float("nan")
+        x[5, 3] = float("-inf")
+        check_product(side, side.t, rows, d_in, d_out, group, xt == "bf16", xt, "fp32", x=x)
+    bf.bf_trusted_status(side.t)
+
+
+@gpu
+@pytest.mark.parametrize("n,d_in,d_out,group,xt", [(150, 6000, 2400, 128, "bf16"), (90, 6000, 2333, 64, "fp32"), (40, 8000, 19000, 128, "bf16"), (17, 16500, 19001, 64, "fp16"),
+                                                  (70, 8000, 19000, 32, "bf16")])
+def test_linear_of_many_outputs_in_a_small_workspace(side, n, d_in, d_out, group, xt):
+    """More rows than the workspace holds at once, and narrower chunks of them, through the products of 128 rows of W at a time."""
+    t = bf.bf_trusted_create(1 << 20, side.stream.cuda_stream)
+    try:
+        check_product(side, t, n, d_in, d_out, group, False, xt, "fp32")
+        bf.bf_trusted_status(t)
+    finally:
+        bf.bf_trusted_destroy(t)
+
+
+@gpu
+@pytest.mark.parametrize("length,D,G", [(20000, 64, 32), (76001, 64, 64), (40000, 128, 64)])
+def test_attention_of_many_splits(side, length, D, G):
+    """One sequence and one key head, so that its tokens are split over more blocks than a warp has lanes."""
+    torch = side.torch
+    pages = -(-length // 64)
+    c = ref.Cache(1, pages + 1, 1, D, G, 64, 1, pages)
+    random_tokens(c, [length], seed=length)
+    d = DeviceCache(side, c)
+    q = torch.randn((6, 2, D), device="cuda").half()
+    check_attention(side, d, 0, None, [1], q[:1], 2, 0, "fp16", starts_given=False)
+    check_attention(side, d, 0, None, [3], q[:3], 2, 15000, "fp16")
+    check_attention(side, d, 0, None, [6], q, 2, 0, "fp16")
+    assert status_of(side) == 0
