@@ -358,7 +358,9 @@ typedef struct {
 
 /* y[i] = W x[i] for n rows: the plaintext counterpart of bf_linear, for projections that stay in the trusted domain (the
  * vocabulary).  Products are of the 4-bit codes themselves, sums in 32 bits, one rounding to the type of y.  x may be any type,
- * y another.  A non-finite x makes its row of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+ * y another: bf16 and fp16 enter whole, fp32 with 22 bits, each but for what lies below 2^-35 of the largest of its row.  Sums are of
+ * codes 0 .. 15, with 8 times the sum of x taken back, so that they round as sums of |x| (15 + 8) scale do.  A non-finite x makes its row
+ * of y non-finite or NaN.  y must not overlap x or W.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
 int bf_q4_linear(bf_trusted* t, const bf_q4_matrix* W, const bf_rows* x, uint32_t n, const bf_rows* y);
 
 /* The encrypted product from the same matrix, on the accelerator (weights are public to it): bf_encode_weights_split and bf_linear with
@@ -374,7 +376,8 @@ int bf_linear_q4(bf_ctx* ctx, const uint64_t* ct_in, uint32_t n_in, const bf_q4_
  * tokens of ONE sequence, for all layers.  An element is low + scale * code, both fp16, per token, head and `group` channels.
  *   pool     device, 16-byte aligned, [n_layers][n_pages][n_kv_heads][bf_kv4_block_bytes]
  *   tables   device, [n_seqs][max_pages]: the page of tokens page_tokens*i .. of a sequence, -1 where there is none
- *   lengths  device, [n_seqs]: tokens of each sequence
+ *   lengths  device, [n_seqs]: tokens of each sequence.  They become more by bf_kv4_grow and 0 by bf_kv4_free; a length that is lowered otherwise
+ *            leaves the pages behind it counted, and the next growth names others in their place
  *   refs     device, [n_pages]: how many tables name a page; 0 = free.  A page that is not full has one owner.
  * A block is page_tokens/16 sub-blocks of 16 tokens, each
  *     key codes     16*D/2 bytes    channel c of token u: nibble c%8 of word (u/8) + 2*(c/32%2) + 4*(c/8%4) + 16*(u%8) + 128*(c/64)

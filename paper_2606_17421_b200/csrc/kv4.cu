@@ -42,7 +42,8 @@ template <int D, int G> struct Sub {
 
 // ------------------------------------------------------------------------------------------------
 // Writing and reading.  One block a (sub-block, head); D / 8 lanes a token, 8 channels a lane, 16 or 32 bytes to a load or store.  Both are
-// bound by what they move; what a sub-block holds is put together in, or taken from, shared memory, so that the cache sees whole lines.
+// bound by issue (two prompts of 4001 tokens, 8 key heads of 128: 55 instructions an element and 64 % of the slots writing, 27 and 76 % reading, 46 us
+// together for 94 MB); what a sub-block holds is put together in, or taken from, shared memory, so that the cache sees whole lines.
 constexpr int IO_THREADS = 128;
 
 __device__ __forceinline__ void load8(float (&x)[8], const bf_rows& r, int64_t at, bool wide) {
@@ -264,8 +265,9 @@ __global__ void __launch_bounds__(IO_THREADS) read_kernel(Cache c, unsigned laye
 //   O^T = V^T (p scale): channels x rows, codes taken the same way; p^T by a transposition in registers, times the scale of each
 //         token and group relative to a power of two that follows them (follow_scales).  The lows are a product of their own, a row a group.
 // Codes lie in the cache as the instructions take them, 16 bytes a lane; asynchronous copies run ATT_STAGES - 1 sub-blocks ahead.
-// Single tokens are bound by issue: about 300 instructions a sub-block of 2.2 KB at D = 128, half of them unpacking and scores, in 55 % of
-// the slots (131072 tokens, 32 query heads: 40 us, 3.5 TB/s); few tokens by the chain of length, table, first copy and joining.
+// Single tokens are bound by issue: 325 instructions a sub-block of 2.2 KB at D = 128 with one group, 436 with four, half of them unpacking and
+// scores, in 54 % of the slots (131072 tokens, 32 query heads: 42 us, 3.4 TB/s); few tokens by the chain of length, table, first copy and joining.
+// Chunks: one block of 8 warps an SM by registers, 39 % of the slots (two chunks of 40 and 64 tokens over 4096, 32 heads).
 constexpr int ATT_WARPS = 8, ATT_STAGES = 4, P_UP = 6;
 constexpr float P_SLACK = 8.f, NO_BASE = __builtin_huge_valf();
 constexpr unsigned PIECE = 128, MOST_SPLITS = 160;          // (what 8 NT rows of them count for fits where the copies were)
@@ -937,9 +939,9 @@ template <int D, int G, int NT> int attention(bf_trusted* t, Att p, unsigned n, 
     if (sets >= (1u << 31) / 64) return BF_ERR_TOO_LARGE;
     // A row's tokens are split while all blocks run at once, as long as a warp keeps eight sub-blocks (four, where that leaves SMs
     // without a block and the tokens are many); and of many sequences, which may differ in length, the long ones into pieces of 128
-    // sub-blocks.  (4096 tokens, 8 key heads: one sequence 11.6 us with four, 14.1 with eight; eight of them 24.1 and 18.1.  700 tokens,
-    // 12 heads: 8.9 and 7.1.  131072 tokens in one wave of blocks 39, in two 48.  32 sequences of 160 to 8000 tokens, 8 key heads: 77 us
-    // with a block each, 67 in pieces of 128, 76 in pieces of 64.)
+    // sub-blocks.  (4096 tokens, 8 key heads: one sequence 13.2 us with four, 15.8 with eight; eight of them 18.2 with either.  700 tokens,
+    // 12 heads: 9.3 and 7.8.  131072 tokens in one wave of blocks 42, in two 55.  32 sequences of 160 to 8000 tokens, 8 key heads: 79 us
+    // with a block each, 62 in pieces of 128, 67 in pieces of 64.)
     const uint64_t n_sb = ((p.window && (uint64_t)p.window + max_q < max_len ? (uint64_t)p.window + max_q : max_len) + 15) / 16;
     const uint64_t slots = (uint64_t)t->n_sm * (NT == 1 ? 2 : 1), wanted = std::max<uint64_t>(1, slots / sets);
     uint64_t splits = std::min(wanted, (n_sb + 8 * ATT_WARPS - 1) / (8 * ATT_WARPS));

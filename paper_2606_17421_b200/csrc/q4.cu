@@ -18,8 +18,9 @@ struct Q4 {
 // exact, sums are fp32; the 8 that a code is offset by enters as the accumulator's start, -8 sum x, and the scale of a
 // group multiplies the 32 to 128 columns' sum in fp32.
 //
-// x is held as fp16 relative to the largest of 256 columns (2^14 .. 2^15), which loses nothing of bf16 or fp16 above
-// 2^-24 of that; fp32 takes two columns of the instruction, x = hi + 2^-11 lo.
+// x is held as fp16 relative to the largest of 256 columns, or of its row where it is laid out once (2^14 .. 2^15), which loses nothing of
+// bf16 or fp16 above 2^-24 of that, and at most 2^-35 of it below; fp32 takes two columns of the instruction, x = hi + 2^-11 lo, 22 bits.
+// Three would hold all 24 and cost half as much again in instructions that are the bound.
 constexpr unsigned SEG = 256, SEG_BLOCKS = SEG / 32;          // columns of a stage; blocks of 32 columns in it
 constexpr unsigned CODE_BYTES = 16 * SEG / 2;                 // 16 rows of a stage
 
@@ -624,8 +625,9 @@ int many_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
     return e == cudaSuccess ? launched(t, "q4_many_kernel") : cuda_failed(t, "q4_many_kernel", e);
 }
 
-// Segments of x that every block makes operands of by itself; more are made once, which costs a launch.  4096 x 4096, 1 / 2 / 4 / 8 rows
-// (16 segments each): in every block 6.1 / 6.9 / 8.7 / 12.4 us, by a kernel of its own 6.7 / 6.7 / 6.7 / 6.7.
+// Segments of x that every block makes operands of by itself; more are made once, which costs a launch.  4096 x 4096, 1 / 2 / 4 rows
+// (16 segments each): in every block 6.0 / 6.8 / 8.6 us, by a kernel of its own 6.6 / 6.7 / 6.6.  Of 14336 columns (56 segments a row) one row: 4096
+// outputs 13.3 either way, 1024 outputs 9.3 and 13.1, 16384 outputs 30.6 and 33.6: there the line is drawn too low.
 constexpr unsigned FEW_UNITS = 32;
 // ------------------------------------------------------------------------------------------------
 // Many rows of W as well: the fifth-generation matrix instructions.  A block of 128 threads has 128 rows of W, a thread a row.  Codes go from
@@ -889,9 +891,16 @@ int wide_launch(bf_trusted* t, const Q4& w, const bf_rows& x, unsigned row0, uns
     return e == cudaSuccess ? launched(t, "q4_wide_kernel") : cuda_failed(t, "q4_wide_kernel", e);
 }
 
-// Rows of W from which blocks of 128 of them are faster than blocks that share the columns out as well.  4096 columns, groups of 128,
-// us with the former and the latter: 128256 rows, 16 / 32 / 64 rows of x 80 and 88 / 105 and 144 / 157 and 220; 4096 rows 29 and 11 /
-// 33 and 24 / 36 and 63.  (Groups of 32 with 64 columns would need more registers for sums than there are.)
+// Rows of W from which products take blocks of 128 of them, in the place of blocks that share the columns out as well.  4096 columns, us with the former and
+// the latter, for 4096 / 19072 / 32768 / 65536 / 128256 rows:
+//   groups of 128  16 rows of x  29, 11 / 34, 23 / 34, 27 / 47, 41 / 80, 89      32  33, 24 / 38, 41 / 39, 42 / 69, 77 / 105, 147
+//                  64            36, 63 / 43, 63 / 44, 64 / 83, 122 / 159, 223
+//   groups of 64   16            37, 11 / 56, 26 / 56, 31 / 72, 49 / 128, 104    32  37, 26 / 58, 56 / 58, 56 / 102, 94 / 163, 165
+//                  64            54, 82 / 73, 84 / 73, 86 / 143, 163 / 275, 304
+//   groups of 32   16            34, 12 / 42, 28 / 43, 34 / 78, 53 / 122, 111    32  40, 29 / 51, 53 / 52, 55 / 100, 93 / 180, 190
+// So the line holds for 64 rows of x, and for 32 but for groups of 64 (4 to 9 % slower than the other up to 65536 rows, 6 to 23 with offsets).  For 16 it
+// is drawn too low: groups of 128 gain from somewhere above 65536 rows only, groups of 64 and 32 nowhere here (up to twice the time).
+// (Groups of 32 with 64 columns would need more registers for sums than there are.)
 template <int G> bool wide_pays(const bf_trusted* t, unsigned d_out, unsigned width) {
     if (width < 16 || TILE / G * width > 128) return false;
     return (d_out + TILE - 1) / TILE >= (unsigned)t->n_sm / (width == 64 ? 8 : 1);
