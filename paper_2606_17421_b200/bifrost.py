@@ -65,13 +65,10 @@ def _where(tensor):
     return device if device >= 0 or not tensor.is_pinned() else None
 
 
-def _common(first, *others):
+def _common(*tensors):
     """The device of all of them; -1 where they are not on one."""
-    device = first.get_device()
-    for x in others:
-        if x.get_device() != device:
-            device = -1
-    return device if device >= 0 else -1 if any(_where(x) is not None for x in (first, *others)) else None
+    devices = {_where(x) for x in tensors} - {None}
+    return devices.pop() if len(devices) == 1 else -1 if devices else None
 
 
 # Descriptors made of tensors (`of`) keep what calls compare with what they read and write: `device`, and of rows `extent`.  Those made of
@@ -79,7 +76,7 @@ def _common(first, *others):
 
 class bf_rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
-    __slots__ = ("device", "extent")
+    __slots__ = ("device", "extent", "__dict__")
 
     @classmethod
     def of(cls, tensor):
@@ -99,7 +96,7 @@ class bf_rows(ctypes.Structure):
 class bf_q4_matrix(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("row_bytes", ctypes.c_uint64),
                 ("group_stride", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("d_in", ctypes.c_uint32), ("group", ctypes.c_uint32)]
-    __slots__ = ("device",)
+    __slots__ = ("device", "__dict__")
 
     @classmethod
     def of(cls, codes, scales, offsets, d_in: int, group: int):
@@ -121,7 +118,7 @@ class bf_q4_matrix(ctypes.Structure):
 class bf_kv4_cache(ctypes.Structure):
     _fields_ = [("pool", ctypes.c_void_p), ("tables", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p)] + \
                [(name, ctypes.c_uint32) for name in ("n_layers", "n_pages", "n_kv_heads", "head_dim", "group", "page_tokens", "n_seqs", "max_pages")]
-    __slots__ = ("device",)
+    __slots__ = ("device", "__dict__")
 
     @classmethod
     def of(cls, pool, tables, lengths, refs, head_dim: int, group: int, page_tokens: int):
@@ -502,7 +499,7 @@ def bf_trusted_create(workspace_bytes: int = 0, cuda_stream: int = 0):
     out = _vp()
     _check_trusted(load().bf_trusted_create(ctypes.byref(out), workspace_bytes, cuda_stream), "bf_trusted_create", None)
     torch = sys.modules.get("torch")
-    out.device = torch.cuda.current_device() if torch else None
+    out.device = torch.cuda.current_device() if torch and torch.cuda.is_available() else None
     return out
 
 

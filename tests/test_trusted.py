@@ -1494,3 +1494,17 @@ def test_attention_of_many_splits(side, length, D, G):
     check_attention(side, d, 0, None, [3], q[:3], 2, 15000, "fp16")
     check_attention(side, d, 0, None, [6], q, 2, 0, "fp16")
     assert status_of(side) == 0
+
+
+def test_descriptors_take_attributes_and_pinned_memory(stand_in):
+    """A caller may hang what has to live as long on a descriptor; memory that the device reaches on the host is let through."""
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(2, 64)
+    rows_, W = bf.bf_rows.of(x), bf.bf_q4_matrix.of(torch.zeros(4, 16, dtype=torch.uint8), torch.zeros(4, 8, dtype=torch.float16), None, 32, 32)
+    c = bf.bf_kv4_cache.of(torch.zeros(1, 2, 1, 64 * 16 + 128, dtype=torch.uint8), *(torch.zeros(s, dtype=torch.int32) for s in ((1, 1), (1,), (2,))), 64, 64, 16)
+    for d in (rows_, W, c, rows(), matrix(), cache()):
+        d.keep = x
+    pinned = Held(x, -1)
+    pinned.is_pinned = lambda: True
+    assert bf.bf_rows.of(pinned).device is None and bf._common(pinned, pinned) is None and bf._common(Held(x), pinned) == 0
+    assert bf._common(Held(x), Held(x, 1)) == -1 and bf._common(Held(x, -1), Held(x, -1)) == -1
