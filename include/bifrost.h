@@ -402,8 +402,8 @@ uint64_t bf_kv4_block_bytes(uint32_t head_dim, uint32_t group, uint32_t page_tok
  * starts[n] are not touched. */
 
 /* Pages for counts[i] (device, int32 [n]; NULL = 1) more tokens of each sequence, lowest free pages first, in the order of the list;
- * lengths grow by that.  A sequence for which no pages are left (OOM), that would exceed its table or is named twice (RANGE: the
- * first one counts) keeps its length; one that needs no new page is always served.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
+ * lengths grow by that.  A sequence for which no pages are left (OOM: what those before it in the list asked for counts, given or not), that would
+ * exceed its table or is named twice (RANGE: the first one counts) keeps its length; one that needs no new page is always served.  Errors: INVALID_ARG, SHAPE, TOO_LARGE, CUDA. */
 int bf_kv4_grow(bf_trusted* t, const bf_kv4_cache* c, const int32_t* seqs, const int32_t* counts, uint32_t n);
 
 /* Quantises rows of k and v ([head][channel], any type) as the last tokens of their sequences in one layer.  Values are clamped to
