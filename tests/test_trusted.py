@@ -1508,3 +1508,36 @@ def test_descriptors_take_attributes_and_pinned_memory(stand_in):
     pinned.is_pinned = lambda: True
     assert bf.bf_rows.of(pinned).device is None and bf._common(pinned, pinned) is None and bf._common(Held(x), pinned) == 0
     assert bf._common(Held(x), Held(x, 1)) == -1 and bf._common(Held(x, -1), Held(x, -1)) == -1
+
+
+@gpu
+def test_runner_and_trusted_half_in_one_graph():
+    """A step captured on the runner's stream takes the half's stream with it: replays go on where eager steps ended."""
+    import torch
+    from paper_2606_17421_b200.runner import TrustedHalf, WorkloadRunner
+    half = TrustedHalf("gpt2_qkv", seqs=2, context=20, room=12, page_tokens=16)
+    R = WorkloadRunner("gpt2_qkv", trusted=half)
+    try:
+        R.step()
+        R.step()
+        torch.cuda.synchronize()
+        assert half.lengths.tolist() == [22, 22]
+        low, logits = R.layers[0]["ct_low"].clone(), half.logits.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=R.stream):
+            R.step()
+        torch.cuda.synchronize()
+        assert half.lengths.tolist() == [22, 22]
+        for i in range(3):
+            R.layers[0]["ct_low"].zero_()
+            half.logits.zero_()
+            half.attended.fill_(float("nan"))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert half.lengths.tolist() == [23 + i] * 2 and int(half.refs.sum()) == 4
+            assert torch.equal(low, R.layers[0]["ct_low"]) and torch.equal(logits, half.logits) and bool(torch.isfinite(half.attended.float()).all())
+        bf.bf_trusted_status(half.ctx)
+    finally:
+        R.close()
+        half.close()
